@@ -334,6 +334,96 @@ int spec_build_labels(const int32_t *tokens, int32_t n_seq, int32_t seq_len, int
 int spec_op_linear_static(int32_t dtype, const void *x, const void *w, float *y, int32_t M, int32_t N,
                           int32_t K, int32_t ctas, void *cuda_stream);
 
+/* ---- 8-bit paged cache ----
+ * A cache of its own beside the bf16 one of a context, for programs that run the layers themselves: half the bytes a token, pages of 16 tokens that several
+ * sequences may share (answers to one prompt), rows that enter it only once they are accepted. Everything lives in the caller's DEVICE memory:
+ *   codes       uint8 [n_layers][n_kv_heads][n_pages][K|V][16 * head_dim], 16-byte aligned
+ *   scales      float [n_layers][n_kv_heads][n_pages][K|V]
+ *   page_table  int32 [max_seqs][pages_per_seq], -1: none
+ *   refs        int32 [n_pages], sequences that hold the page (0: free)
+ *   lens        int32 [max_seqs], tokens of each sequence
+ *   status      int32 [4], zero: set by kernels that meet a sequence, page or row number out of range (code ST_BOUNDS = 2, place, detail); such an entry is skipped
+ * An empty cache is page_table -1, the rest 0. A value is code * scale of its block; a code is an int8 in -127..127 or an e4m3 byte. K block: [token / 8][dim / 16][token % 8][dim % 16]; V
+ * block: [dim][place], token t of the page at place 4 ((t % 8) / 2) + 2 (t / 8) + t % 2. head_dim is 64 or 128.
+ * All calls are asynchronous on `cuda_stream`, return SPEC_OK or SPEC_E_* (spec_last_error(NULL) says why) and allocate nothing; an empty one (no rows, no
+ * sequences) does nothing. Calls that change a cache and calls that use it must be ordered by their caller (one stream, or events). `seqs`: DEVICE
+ * int32 [batch], the sequence of each group, each at most once a call; NULL: 0 .. batch - 1. Rows of a pass: those of group b are row_offsets[b] .. row_offsets[b + 1] - 1 (DEVICE
+ * int32 [batch + 1], ascending), or rows / batch each with NULL. Strides are in elements; a head's values are contiguous. */
+enum { SPEC_CACHE_INT8 = 0, SPEC_CACHE_E4M3 = 1 };
+enum { SPEC_TYPE_F32 = 0, SPEC_TYPE_BF16 = 1, SPEC_TYPE_F16 = 2 };
+
+typedef struct {
+  int32_t n_layers, n_kv_heads, head_dim, n_pages, max_seqs, pages_per_seq, format;
+  uint8_t *codes;
+  float *scales;
+  int32_t *page_table, *refs, *lens, *status;
+} spec_cache;
+
+/* Attention of the rows of a pass: out_i = sum_j w_ij v_j / sum_j w_ij, w_ij = exp(scale q_i.k_j), over all lens[sequence] cached tokens and the rows j of the pass, of the same
+ * sequence, that row i sees: bit j % 32 of mask[row][j / 32] (DEVICE uint32 [rows][mask_words]; j counts within the sequence's rows), or j <= i with mask NULL.
+ * k and v are the pass's own rows [rows][n_kv_heads][head_dim], not yet in the cache; query head h uses kv head h / (n_heads / n_kv_heads). out: [rows][n_heads][head_dim]
+ * contiguous, of the operands' type; lse: float [rows][n_heads], log sum_j w_ij, or NULL. A row that sees nothing gives zeros and -infinity. Values of rows that a row does not
+ * see do not reach it, whatever they are. max_rows: at least the rows of any sequence. bf16 and f16 run on the tensor cores (rows must start on 16-byte boundaries;
+ * softmax weights are rounded to the operand type before they meet v), f32 on CUDA cores.
+ * scratch: DEVICE, spec_cache_attention_scratch() bytes, 16-byte aligned, ZERO before its first use, not shared by calls that may overlap. */
+typedef struct {
+  const void *q, *k, *v;
+  void *out;
+  float *lse;
+  const int32_t *seqs, *row_offsets;
+  const uint32_t *mask;
+  int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int32_t type, rows, batch, n_heads, layer, max_rows, mask_words;
+  float scale;
+} spec_attention_args;
+size_t spec_cache_attention_scratch(const spec_cache *cache, int32_t n_heads, int32_t batch, int32_t max_rows);
+int spec_cache_attention(const spec_cache *cache, const spec_attention_args *args, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/* Rows into the cache, of layers layer0 .. layer0 + layers - 1 at once: the rows path[b][0 .. counts[b] - 1] of group b (DEVICE int32 [batch][max_count], numbers within the
+ * group's rows; NULL: its first counts[b]) become the sequence's LAST counts[b] tokens, for which spec_cache_reserve has made room. counts: DEVICE, what it granted. Per
+ * block, scale = max(scale before if the page held tokens, largest finite magnitude / 127 (int8) or 448 (e4m3)), code = round(value / scale), to even; older codes of the page are
+ * rounded again where the scale grew; infinities are held at the largest code, NaN becomes 0. A block whose largest magnitude is below 2^-100 is zeros with scale 0. */
+typedef struct {
+  const void *k, *v;               /* [layers][rows][n_kv_heads][head_dim] */
+  const int32_t *seqs, *row_offsets, *counts, *path;
+  int64_t k_layer_stride, k_row_stride, k_head_stride, v_layer_stride, v_row_stride, v_head_stride;
+  int32_t type, rows, batch, layer0, layers, max_count;
+} spec_store_args;
+int spec_cache_store(const spec_cache *cache, const spec_store_args *args, void *cuda_stream);
+
+/* Tokens start[b] .. start[b] + window - 1 (start NULL: 0) of every group and layer, decoded: k, v [layers][batch][window][n_kv_heads][head_dim] contiguous; zeros past the end. */
+typedef struct {
+  void *k, *v;
+  const int32_t *seqs, *start;
+  int32_t type, batch, window, layer0, layers;
+} spec_read_args;
+int spec_cache_read(const spec_cache *cache, const spec_read_args *args, void *cuda_stream);
+
+/* Pages. fork: sequence dst[b], which must be empty, becomes a second holder of all pages of src[b]. reserve: room for counts[b] more tokens of each sequence (lens grows), new
+ * pages being the lowest free ones in the order of the call; a last page that is partial and shared is copied first. granted[b] (DEVICE) is counts[b], or 0 where the pool or the
+ * table has no room. truncate: sequences keep their first keep[b] tokens (NULL: none), pages that nobody holds any more are free. compact: the pages in use move to the numbers below
+ * their count, which *used (DEVICE) receives. A group's pages are numbers of all layers. scratch: DEVICE, spec_cache_scratch_bytes() bytes, 16-byte aligned, any content. batch <= 1024 for reserve. */
+size_t spec_cache_scratch_bytes(const spec_cache *cache);
+int spec_cache_fork(const spec_cache *cache, int32_t batch, const int32_t *src, const int32_t *dst, void *cuda_stream);
+int spec_cache_reserve(const spec_cache *cache, int32_t batch, const int32_t *seqs, const int32_t *counts, int32_t *granted, void *scratch, size_t scratch_bytes, void *cuda_stream);
+int spec_cache_truncate(const spec_cache *cache, int32_t batch, const int32_t *seqs, const int32_t *keep, void *cuda_stream);
+int spec_cache_compact(const spec_cache *cache, int32_t *used, void *scratch, size_t scratch_bytes, void *cuda_stream);
+
+/* Rotary positions of q [rows][n_heads][head_dim] and k [rows][n_kv_heads][head_dim]: the first rot_dim values of a head turn in pairs (x[i], x[i + rot_dim / 2]), or (x[2 i], x[2 i + 1]) with
+ * `interleaved`, by the angle whose (cos, sin) is table[positions[row]][i]; the rest, and v [rows][n_v_heads][head_dim], is cast. Inputs of in_type with strides, outputs of out_type, contiguous. A
+ * row whose position is outside 0 .. span - 1 becomes NaN. Any of the three may have 0 heads.
+ * spec_rotary_table fills table, float [span][half][2], with (cos, sin)(position * freq[i]) * gain, computed in double; freq: DEVICE double [half]. */
+typedef struct {
+  const void *q, *k, *v;
+  void *q_out, *k_out, *v_out;
+  const int32_t *positions;
+  const float *table;
+  int64_t q_row_stride, q_head_stride, k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  int32_t in_type, out_type, rows, n_heads, n_kv_heads, n_v_heads, head_dim, rot_dim, span, interleaved;
+} spec_rotary_args;
+int spec_rotary(const spec_rotary_args *args, void *cuda_stream);
+int spec_rotary_table(float *table, const double *freq, int32_t span, int32_t half, double gain, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,332 @@
+"""8-bit paged cache, attention over it and rotary positions: the Python side of the spec_cache_* and spec_rotary* entry points.
+
+Argument checks and marshalling only; every operation is a CUDA kernel of the library, enqueued on the current stream of the
+cache's device. A cache's tensors are public: `codes`, `scales`, `page_table`, `refs`, `lens` (see include/spec_decode.h for the layout).
+
+A step of a program that runs the layers itself:
+
+    q, k, v = spec_rotary(q, k, v, positions, table)                    # per layer, out of the projection's output
+    o = cache.attention(layer, q, k, v, mask=tree_mask)                 # cached tokens + the pass's own rows
+    ...                                                                 # accept a path
+    granted = cache.reserve(counts)                                     # pages for the accepted tokens, all layers
+    cache.store(k_all_layers, v_all_layers, granted, path=path)
+"""
+import ctypes as C
+import functools
+import math
+from typing import Optional, Tuple
+
+from .binding import SpecError, _torch, load_library
+
+PAGE = 16
+FORMATS = {"int8": 0, "e4m3": 1}
+
+
+class _Cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_kv_heads", "head_dim", "n_pages", "max_seqs", "pages_per_seq", "format")] + \
+               [(n, C.c_void_p) for n in ("codes", "scales", "page_table", "refs", "lens", "status")]
+
+
+class _AttentionArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "out", "lse", "seqs", "row_offsets", "mask")] + \
+               [(n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head")] + \
+               [(n, C.c_int32) for n in ("type", "rows", "batch", "n_heads", "layer", "max_rows", "mask_words")] + [("scale", C.c_float)]
+
+
+class _StoreArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "seqs", "row_offsets", "counts", "path")] + \
+               [(n, C.c_int64) for n in ("k_layer", "k_row", "k_head", "v_layer", "v_row", "v_head")] + \
+               [(n, C.c_int32) for n in ("type", "rows", "batch", "layer0", "layers", "max_count")]
+
+
+class _ReadArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "seqs", "start")] + [(n, C.c_int32) for n in ("type", "batch", "window", "layer0", "layers")]
+
+
+class _RotaryArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out", "k_out", "v_out", "positions", "table")] + \
+               [(n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head")] + \
+               [(n, C.c_int32) for n in ("in_type", "out_type", "rows", "n_heads", "n_kv_heads", "n_v_heads", "head_dim", "rot_dim", "span", "interleaved")]
+
+
+@functools.lru_cache(maxsize=1)
+def _library():
+    """(library, torch, raw stream of a device ordinal, {torch dtype: the library's type})"""
+    torch, raw_stream = _torch()
+    lib = load_library()
+    p, i, size = C.c_void_p, C.c_int32, C.c_size_t
+    for name, res, args in (
+            ("spec_cache_attention", C.c_int, [p, p, p, size, p]), ("spec_cache_attention_scratch", size, [p, i, i, i]),
+            ("spec_cache_store", C.c_int, [p, p, p]), ("spec_cache_read", C.c_int, [p, p, p]), ("spec_cache_scratch_bytes", size, [p]),
+            ("spec_cache_fork", C.c_int, [p, i, p, p, p]), ("spec_cache_reserve", C.c_int, [p, i, p, p, p, p, size, p]),
+            ("spec_cache_truncate", C.c_int, [p, i, p, p, p]), ("spec_cache_compact", C.c_int, [p, p, p, size, p]),
+            ("spec_rotary", C.c_int, [p, p]), ("spec_rotary_table", C.c_int, [p, p, i, i, C.c_double, p])):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = res, args
+    return lib, torch, raw_stream, {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _raise(rc: int):
+    raise SpecError(rc, load_library().spec_last_error(None).decode())
+
+
+def _bad(text: str):
+    raise SpecError(-1, text)
+
+
+class SpecCache:
+    """Handle of an 8-bit paged cache. Owns its tensors (or borrows those given to from_tensors) and, per stream that uses it, a workspace."""
+
+    def __init__(self, n_layers: int, n_kv_heads: int, head_dim: int, n_pages: int, max_seqs: int, pages_per_seq: int, fmt: str = "int8", device="cuda:0"):
+        import torch
+        if min(n_layers, n_kv_heads, n_pages, max_seqs, pages_per_seq) < 1 or head_dim not in (64, 128) or fmt not in FORMATS:
+            _bad("SpecCache: sizes must be positive, head_dim 64 or 128, fmt int8 or e4m3")
+        codes = torch.zeros((n_layers, n_kv_heads, n_pages, 2, PAGE * head_dim), dtype=torch.uint8, device=device)
+        scales = torch.zeros((n_layers, n_kv_heads, n_pages, 2), dtype=torch.float32, device=device)
+        table = torch.full((max_seqs, pages_per_seq), -1, dtype=torch.int32, device=device)
+        self._take(codes, scales, table, torch.zeros(n_pages, dtype=torch.int32, device=device), torch.zeros(max_seqs, dtype=torch.int32, device=device), fmt)
+
+    @classmethod
+    def from_tensors(cls, codes, scales, page_table, refs, lens, fmt: str = "int8") -> "SpecCache":
+        """A handle on tensors laid out as include/spec_decode.h says (they are used in place)."""
+        self = cls.__new__(cls)
+        self._take(codes, scales, page_table, refs, lens, fmt)
+        return self
+
+    def _take(self, codes, scales, page_table, refs, lens, fmt):
+        import torch
+        if fmt not in FORMATS:
+            _bad("SpecCache: fmt must be int8 or e4m3")
+        L, kv, pages, two, block = codes.shape
+        D = block // PAGE
+        for t, dt, shape in ((codes, torch.uint8, (L, kv, pages, 2, PAGE * D)), (scales, torch.float32, (L, kv, pages, 2)), (page_table, torch.int32, tuple(page_table.shape)),
+                             (refs, torch.int32, (pages,)), (lens, torch.int32, (page_table.shape[0],))):
+            if t.dtype != dt or tuple(t.shape) != shape or not t.is_contiguous() or not t.is_cuda or t.device != codes.device:
+                _bad(f"SpecCache: expected a contiguous {dt} CUDA tensor of shape {shape}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        self.codes, self.scales, self.page_table, self.refs, self.lens, self.fmt = codes, scales, page_table, refs, lens, fmt
+        self.device, self.n_layers, self.n_kv_heads, self.head_dim = codes.device, L, kv, D
+        self.status = torch.zeros(4, dtype=torch.int32, device=self.device)
+        self._c = _Cache(L, kv, D, pages, page_table.shape[0], page_table.shape[1], FORMATS[fmt], codes.data_ptr(), scales.data_ptr(), page_table.data_ptr(), refs.data_ptr(),
+                         lens.data_ptr(), self.status.data_ptr())
+        self._p = C.addressof(self._c)
+        self.lib, self._torch, self._raw_stream, self._types = _library()
+        self._index = self.device.index
+        self._work = {}                          # workspaces by (stream, kind): calls on different streams may overlap
+        self._sizes = {}
+        if not self.lib.spec_cache_scratch_bytes(self._p):
+            _bad("SpecCache: " + ("head_dim must be 64 or 128" if D not in (64, 128) else "sizes out of range"))
+
+    # ---- helpers
+    def _workspace(self, stream: int, kind: str, need: int):
+        w = self._work.get((stream, kind))
+        if w is None or w.numel() < need:
+            w = self._torch.zeros(need, dtype=self._torch.uint8, device=self.device)
+            self._work[(stream, kind)] = w
+        return w.data_ptr()
+
+    def _ints(self, t, n: Optional[int], what: str):
+        """Address of an int32 vector on the cache's device (None: 0)."""
+        if t is None:
+            return None
+        if t.dtype != self._torch.int32 or t.device != self.device or not t.is_contiguous() or (n is not None and t.numel() != n):
+            _bad(f"{what}: expected a contiguous int32 tensor{'' if n is None else f' of {n} values'} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return t.data_ptr()
+
+    def _rows(self, t, heads, what: str, lead: int = 0):
+        if t.dim() != 3 + lead or t.shape[-1] != self.head_dim or (heads is not None and t.shape[-2] != heads) or t.stride(-1) != 1 or t.device != self.device or t.dtype not in self._types:
+            _bad(f"{what}: expected {'[layers, ' if lead else '['}rows, {'heads' if heads is None else heads}, {self.head_dim}] with contiguous last dimension on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+    def check(self):
+        """Synchronises; raises if a kernel met a sequence, page or row number out of range since the last check (and clears the mark)."""
+        s = self.status.tolist()
+        if s[0]:
+            self.status.zero_()
+            raise SpecError(-1, f"cache: a number out of range at place {s[1]} (value {s[2]})")
+
+    # ---- operations
+    def attention(self, layer: int, q, k, v, *, batch: int = 1, row_offsets=None, max_rows: Optional[int] = None, seqs=None, mask=None, scale: Optional[float] = None,
+                  lse: bool = False, out=None):
+        """softmax(scale q k^T) v of the rows of a pass over their sequences' cached tokens and the pass's own rows k, v.
+
+        q [rows, heads, D], k and v [rows, kv heads, D] (bf16, f16 or f32, all alike; any row and head strides that keep rows on 16-byte boundaries). `batch` groups of rows
+        / batch rows each, or given by row_offsets (int32 [batch + 1] on the device; then max_rows bounds the rows of a group). seqs: the groups' sequences (0 .. batch - 1).
+        mask: int32 [rows, words], bit j of a row: it sees row j of its group; None: causal. Returns out, or (out, lse) with lse=True."""
+        lib, torch = self.lib, self._torch
+        rows, heads = q.shape[0], q.shape[1]
+        self._rows(q, None, "attention: q")
+        self._rows(k, self.n_kv_heads, "attention: k")
+        self._rows(v, self.n_kv_heads, "attention: v")
+        if not q.dtype == k.dtype == v.dtype or k.shape[0] != rows or v.shape[0] != rows:
+            _bad("attention: q, k and v must have the same rows and type")
+        if row_offsets is None:
+            if batch < 1 or rows % batch:
+                _bad(f"attention: {rows} rows do not divide among {batch} groups")
+            max_rows = max(1, rows // batch)
+        elif max_rows is None:
+            _bad("attention: row_offsets needs max_rows")
+        words = 0
+        if mask is not None:
+            if mask.dim() != 2 or mask.shape[0] != rows or mask.dtype != torch.int32 or mask.device != self.device or not mask.is_contiguous():
+                _bad("attention: mask must be a contiguous int32 tensor [rows, words] on the cache's device")
+            words = mask.shape[1]
+        if out is None:
+            out = torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=self.device)
+        elif out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous() or out.device != self.device:
+            _bad("attention: out must be contiguous, of q's shape and type")
+        sums = torch.empty((rows, heads), dtype=torch.float32, device=self.device) if lse else None
+        qs, ks, vs = q.stride(), k.stride(), v.stride()
+        a = _AttentionArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), sums.data_ptr() if lse else None, self._ints(seqs, batch, "attention: seqs"),
+                           self._ints(row_offsets, batch + 1, "attention: row_offsets"), mask.data_ptr() if words else None, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1],
+                           self._types[q.dtype], rows, batch, heads, layer, max_rows, words, 1.0 / math.sqrt(self.head_dim) if scale is None else scale)
+        key = (heads, batch, max_rows)
+        need = self._sizes.get(key)
+        if need is None:
+            need = self._sizes[key] = lib.spec_cache_attention_scratch(self._p, heads, batch, max_rows)
+        stream = self._raw_stream(self._index)
+        rc = lib.spec_cache_attention(self._p, C.addressof(a), self._workspace(stream, "attention", need), need, stream)
+        if rc:
+            _raise(rc)
+        return (out, sums) if lse else out
+
+    def store(self, k, v, counts, *, batch: Optional[int] = None, row_offsets=None, seqs=None, path=None, max_count: Optional[int] = None, layer0: int = 0):
+        """Rows k, v [layers, rows, kv heads, D] of a pass into the cache: the rows path[b][:counts[b]] of group b (its first counts[b] without a path) become the last counts[b] tokens of
+        its sequence, for which reserve() has made room. counts: int32 [batch] on the device, what reserve() returned. path: int32 [batch, longest]; without one max_count bounds the counts
+        (default: the rows of a group)."""
+        self._rows(k, self.n_kv_heads, "store: k", 1)
+        self._rows(v, self.n_kv_heads, "store: v", 1)
+        layers, rows = k.shape[0], k.shape[1]
+        if k.dtype != v.dtype or v.shape != k.shape:
+            _bad("store: k and v must have the same shape and type")
+        batch = counts.numel() if batch is None else batch
+        if path is not None:
+            if path.dim() != 2 or path.shape[0] != batch:
+                _bad("store: path must be int32 [batch, longest]")
+            max_count = path.shape[1]
+        elif max_count is None:
+            if row_offsets is not None:
+                _bad("store: row_offsets without a path needs max_count")
+            max_count = rows // max(batch, 1)
+        if row_offsets is None and batch and rows % batch:
+            _bad(f"store: {rows} rows do not divide among {batch} groups")
+        ks, vs = k.stride(), v.stride()
+        a = _StoreArgs(k.data_ptr(), v.data_ptr(), self._ints(seqs, batch, "store: seqs"), self._ints(row_offsets, batch + 1, "store: row_offsets"), self._ints(counts, batch, "store: counts"),
+                       self._ints(path, None, "store: path"), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], self._types[k.dtype], rows, batch, layer0, layers, max_count)
+        rc = self.lib.spec_cache_store(self._p, C.addressof(a), self._raw_stream(self._index))
+        if rc:
+            _raise(rc)
+
+    def read(self, start, window: int, *, batch: Optional[int] = None, seqs=None, dtype=None, layer0: int = 0, layers: Optional[int] = None):
+        """(k, v) [layers, batch, window, kv heads, D] of tokens start[b] .. start[b] + window - 1 (start None: 0), decoded; zeros past a sequence's end."""
+        torch = self._torch
+        batch = (start.numel() if start is not None else self.lens.numel()) if batch is None else batch
+        layers = self.n_layers - layer0 if layers is None else layers
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in self._types:
+            _bad("read: dtype must be bfloat16, float16 or float32")
+        k, v = (torch.empty((max(layers, 0), batch, max(window, 0), self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device) for _ in "kv")
+        a = _ReadArgs(k.data_ptr(), v.data_ptr(), self._ints(seqs, batch, "read: seqs"), self._ints(start, batch, "read: start"), self._types[dtype], batch, window, layer0, layers)
+        rc = self.lib.spec_cache_read(self._p, C.addressof(a), self._raw_stream(self._index))
+        if rc:
+            _raise(rc)
+        return k, v
+
+    def fork(self, src, dst):
+        """Sequences dst[b], which must be empty, share all pages of sequences src[b] (int32 tensors on the device)."""
+        rc = self.lib.spec_cache_fork(self._p, dst.numel(), self._ints(src, dst.numel(), "fork: src"), self._ints(dst, None, "fork: dst"), self._raw_stream(self._index))
+        if rc:
+            _raise(rc)
+
+    def reserve(self, counts, *, seqs=None):
+        """Room for counts[b] more tokens of each sequence; returns the counts granted (a sequence gets all or, where pool or table are full, nothing)."""
+        granted = self._torch.empty_like(counts)
+        batch = counts.numel()
+        stream = self._raw_stream(self._index)
+        need = self._scratch_bytes()
+        rc = self.lib.spec_cache_reserve(self._p, batch, self._ints(seqs, batch, "reserve: seqs"), self._ints(counts, batch, "reserve: counts"), granted.data_ptr(),
+                                         self._workspace(stream, "pages", need), need, stream)
+        if rc:
+            _raise(rc)
+        return granted
+
+    def truncate(self, keep=None, *, seqs=None):
+        """Sequences keep their first keep[b] tokens (None: nothing; then seqs names them, or all are emptied); pages that nobody holds any more are free."""
+        batch = keep.numel() if keep is not None else seqs.numel() if seqs is not None else self.lens.numel()
+        rc = self.lib.spec_cache_truncate(self._p, batch, self._ints(seqs, batch, "truncate: seqs"), self._ints(keep, batch, "truncate: keep"), self._raw_stream(self._index))
+        if rc:
+            _raise(rc)
+
+    def compact(self):
+        """Moves the pages in use to the lowest numbers; returns how many there are (int32 [1] on the device)."""
+        used = self._torch.empty(1, dtype=self._torch.int32, device=self.device)
+        stream = self._raw_stream(self._index)
+        need = self._scratch_bytes()
+        rc = self.lib.spec_cache_compact(self._p, used.data_ptr(), self._workspace(stream, "pages", need), need, stream)
+        if rc:
+            _raise(rc)
+        return used
+
+    def _scratch_bytes(self) -> int:
+        n = self._sizes.get("pages")
+        if n is None:
+            n = self._sizes["pages"] = self.lib.spec_cache_scratch_bytes(self._p)
+        return n
+
+
+def spec_rotary(q, k, v, positions, table, *, interleaved: bool = False, dtype=None) -> Tuple:
+    """Rotated q and k, and v cast, all contiguous in `dtype` (default: q's). q [rows, heads, D], k and v [rows, kv heads, D] may be strided views of one projection's output (v may
+    be None); positions int32 [rows]; table float32 [span, rot / 2, 2] from spec_rotary_table: the first `rot` dims of every head of q and k turn."""
+    lib, torch, raw_stream, types = _library()
+    rows, D = q.shape[0], q.shape[-1]
+    dtype = q.dtype if dtype is None else dtype
+    for t, what in ((q, "q"), (k, "k"), (v, "v")):
+        if t is not None and (t.dim() != 3 or t.shape[0] != rows or t.shape[2] != D or t.dtype != q.dtype or t.stride(2) != 1 or t.device != q.device):
+            _bad(f"spec_rotary: {what} must be [rows, heads, D] with contiguous last dimension, like q")
+    if q.dtype not in types or dtype not in types:
+        _bad("spec_rotary: types must be float32, bfloat16 or float16")
+    if positions.dtype != torch.int32 or positions.numel() != rows or not positions.is_contiguous() or positions.device != q.device:
+        _bad("spec_rotary: positions must be a contiguous int32 tensor, one value a row")
+    if table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous() or table.device != q.device:
+        _bad("spec_rotary: table must be a contiguous float32 tensor [span, rot / 2, 2]")
+    H, kv, kvv, device = q.shape[1], k.shape[1], v.shape[1] if v is not None else 0, q.device
+    qo = torch.empty((rows, H, D), dtype=dtype, device=device)
+    ko = torch.empty((rows, kv, D), dtype=dtype, device=device)
+    vo = torch.empty((rows, kvv, D), dtype=dtype, device=device) if v is not None else None
+    qs, ks, vs = q.stride(), k.stride(), v.stride() if v is not None else (0, 0)
+    a = _RotaryArgs(q.data_ptr(), k.data_ptr(), v.data_ptr() if v is not None else None, qo.data_ptr(), ko.data_ptr(), vo.data_ptr() if v is not None else None, positions.data_ptr(),
+                    table.data_ptr(), qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], types[q.dtype], types[dtype], rows, H, kv, kvv, D, 2 * table.shape[1], table.shape[0], int(interleaved))
+    rc = lib.spec_rotary(C.addressof(a), raw_stream(device.index))
+    if rc:
+        _raise(rc)
+    return qo, ko, vo
+
+
+def rotary_frequencies(rot: int, base: float, scaling: str = "none", factor: float = 1.0, original: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(angular step of each of the rot / 2 pairs, gain of cos and sin). scaling: "none"; "linear": positions / factor; "ntk": base * factor ** (rot / (rot - 2));
+    "yarn": pairs that make fewer than beta_slow turns over the `original` context slow down by factor, those above beta_fast keep their pace, a ramp between, gain 0.1 ln(factor) + 1."""
+    if rot < 2 or rot % 2 or base <= 0 or factor <= 0 or scaling not in ("none", "linear", "ntk", "yarn") or (scaling == "ntk" and rot < 4) or (scaling == "yarn" and (original < 1 or base <= 1)):
+        _bad("rotary_frequencies: unsupported arguments")
+    if scaling == "ntk":
+        base *= factor ** (rot / (rot - 2))
+    f = [base ** (-2.0 * i / rot) for i in range(rot // 2)]
+    if scaling == "linear":
+        f = [x / factor for x in f]
+    if scaling != "yarn":
+        return f, 1.0
+    turn = lambda beta: rot * math.log(original / (beta * 2 * math.pi)) / (2 * math.log(base))  # noqa: E731
+    low, high = max(math.floor(turn(beta_fast)), 0), min(math.ceil(turn(beta_slow)), rot - 1)
+    ramp = [min(max((i - low) / max(high - low, 1e-3), 0.0), 1.0) for i in range(rot // 2)]
+    return [x * (1 - r) + x / factor * r for x, r in zip(f, ramp)], 0.1 * math.log(factor) + 1.0
+
+
+def spec_rotary_table(span: int, rot: int, base: float, scaling: str = "none", factor: float = 1.0, original: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda:0"):
+    """Table [span, rot / 2, 2] of (cos, sin) for spec_rotary, angles and functions in double; see rotary_frequencies for the scalings."""
+    lib, torch, raw_stream, _ = _library()
+    if span < 1:
+        _bad("spec_rotary_table: span must be positive")
+    freq, gain = rotary_frequencies(rot, base, scaling, factor, original, beta_fast, beta_slow)
+    f = torch.tensor(freq, dtype=torch.float64, device=device)
+    table = torch.empty((span, rot // 2, 2), dtype=torch.float32, device=f.device)
+    rc = lib.spec_rotary_table(table.data_ptr(), f.data_ptr(), span, rot // 2, gain, raw_stream(f.device.index))
+    if rc:
+        _raise(rc)
+    return table

@@ -1,0 +1,233 @@
+// C ABI of the 8-bit paged cache: argument checks and launches. All work is enqueued on the caller's stream; nothing is allocated,
+// nothing waits. Device-side findings (a page or sequence number out of range) go to the cache's status word.
+#include <stdio.h>
+#include <stdarg.h>
+
+#include "cache_attention.cuh"
+#include "cache_common.cuh"
+#include "cache_pages.cuh"
+#include "cache_rows.cuh"
+
+namespace spec {
+void set_last_error(const char* text) noexcept;   // spec_api.cu
+}
+
+using namespace spec;
+
+namespace {
+
+int fail(int code, const char* fmt, ...) {
+  char text[256];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(text, sizeof text, fmt, ap);
+  va_end(ap);
+  set_last_error(text);
+  return code;
+}
+
+int launched(const char* what) {
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? SPEC_OK : fail(SPEC_E_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// nullptr if the cache can be used, else what is wrong with it
+const char* cache_fault(const spec_cache* c) {
+  if (!c || !c->codes || !c->scales || !c->page_table || !c->refs || !c->lens || !c->status) return "null cache or cache pointer";
+  if (c->n_layers < 1 || c->n_kv_heads < 1 || c->n_pages < 1 || c->max_seqs < 1 || c->pages_per_seq < 1) return "non-positive cache size";
+  if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
+  if (c->format != SPEC_CACHE_INT8 && c->format != SPEC_CACHE_E4M3) return "format must be SPEC_CACHE_INT8 or SPEC_CACHE_E4M3";
+  if (c->n_pages > (1 << 27) || c->pages_per_seq > (1 << 26)) return "cache too large (2^27 pages, 2^30 tokens a sequence)";
+  if (!aligned(c->codes, 16)) return "codes must be 16-byte aligned";
+  return nullptr;
+}
+
+CacheView view(const spec_cache* c) {
+  return CacheView{c->codes, c->scales, c->page_table, c->refs, c->lens, c->status, c->n_layers, c->n_kv_heads, c->head_dim, c->n_pages, c->max_seqs, c->pages_per_seq};
+}
+
+int elem_size(int dtype) { return dtype == SPEC_TYPE_F32 ? 4 : 2; }
+bool known_type(int dtype) { return dtype == SPEC_TYPE_F32 || dtype == SPEC_TYPE_BF16 || dtype == SPEC_TYPE_F16; }
+
+template <typename F> auto by_type(int dtype, F f) {
+  if (dtype == SPEC_TYPE_F32) return f(float{});
+  if (dtype == SPEC_TYPE_BF16) return f(bf16{});
+  return f(f16{});
+}
+template <int V> struct Int { static constexpr int value = V; };
+// f(head dim, format) as compile-time values
+template <typename F> auto by_shape(const spec_cache* c, F f) {
+  if (c->head_dim == 128) return c->format == SPEC_CACHE_INT8 ? f(Int<128>{}, Int<CACHE_INT8>{}) : f(Int<128>{}, Int<CACHE_E4M3>{});
+  return c->format == SPEC_CACHE_INT8 ? f(Int<64>{}, Int<CACHE_INT8>{}) : f(Int<64>{}, Int<CACHE_E4M3>{});
+}
+
+}  // namespace
+
+extern "C" {
+
+int spec_rotary_table(float* table, const double* freq, int32_t span, int32_t half, double gain, void* cuda_stream) {
+  if (!table || !freq || span < 1 || half < 1) return fail(SPEC_E_BADARG, "spec_rotary_table: null pointer or non-positive size");
+  const long long n = (long long)span * half;
+  rotary_table_kernel<<<(unsigned)((n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+      reinterpret_cast<float2*>(table), freq, span, half, gain);
+  return launched("spec_rotary_table");
+}
+
+int spec_rotary(const spec_rotary_args* r, void* cuda_stream) {
+  if (!r) return fail(SPEC_E_BADARG, "spec_rotary: null argument");
+  if (r->rows == 0) return SPEC_OK;
+  if (r->rows < 0 || r->n_heads < 0 || r->n_kv_heads < 0 || r->n_v_heads < 0 || r->head_dim < 2 || r->head_dim % 2 || r->head_dim > 1024 || r->rot_dim < 2 || r->rot_dim % 2 || r->rot_dim > r->head_dim || r->span < 1)
+    return fail(SPEC_E_BADARG, "spec_rotary: unsupported sizes (%d rows, %d + %d + %d heads of %d, %d rotated, span %d)", r->rows, r->n_heads, r->n_kv_heads, r->n_v_heads, r->head_dim, r->rot_dim, r->span);
+  if ((r->n_heads && (!r->q || !r->q_out)) || (r->n_kv_heads && (!r->k || !r->k_out)) || (r->n_v_heads && (!r->v || !r->v_out)) || !r->positions || !r->table)
+    return fail(SPEC_E_BADARG, "spec_rotary: null pointer");
+  if (!known_type(r->in_type) || !known_type(r->out_type)) return fail(SPEC_E_BADARG, "spec_rotary: unknown type");
+  RotaryArgs a{r->q, r->k, r->v, r->q_row_stride, r->k_row_stride, r->v_row_stride, r->q_head_stride, r->k_head_stride, r->v_head_stride, r->q_out, r->k_out, r->v_out,
+               r->positions, reinterpret_cast<const float2*>(r->table), r->rows, r->n_heads, r->n_kv_heads, r->n_v_heads, r->head_dim, r->rot_dim, r->span};
+  // four pairs a thread where every access of four elements is aligned
+  const size_t vi = 4 * elem_size(r->in_type), vo = 4 * elem_size(r->out_type);
+  const bool strides = r->q_row_stride % 4 == 0 && r->q_head_stride % 4 == 0 && r->k_row_stride % 4 == 0 && r->k_head_stride % 4 == 0 && r->v_row_stride % 4 == 0 && r->v_head_stride % 4 == 0;
+  const bool wide = r->head_dim % 8 == 0 && r->rot_dim % 8 == 0 && strides && aligned(r->q, vi) && aligned(r->k, vi) && aligned(r->v, vi) && aligned(r->q_out, vo) && aligned(r->k_out, vo) && aligned(r->v_out, vo);
+  const int per_head = r->rot_dim / 2 / (wide ? 4 : 1), sweep = ROT_THREADS / per_head > 0 ? ROT_THREADS / per_head : 1;
+  const int heads = r->n_heads + r->n_kv_heads;
+  // parts of the heads so that a few rows, too, fill the SMs; a block keeps ROT_HEADS sweeps where there are rows enough
+  int parts = (heads + sweep * ROT_HEADS - 1) / (sweep * ROT_HEADS);
+  while (parts * sweep < heads && (long long)parts * r->rows < 148 * 8) ++parts;
+  if (parts < 1) parts = 1;
+  const dim3 grid(r->rows, parts < 65535 ? parts : 65535);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  by_type(r->in_type, [&](auto ti) {
+    by_type(r->out_type, [&](auto to) {
+      typedef decltype(ti) TI;
+      typedef decltype(to) TO;
+      if (wide) r->interleaved ? rotary_kernel<TI, TO, true, 4><<<grid, ROT_THREADS, 0, st>>>(a) : rotary_kernel<TI, TO, false, 4><<<grid, ROT_THREADS, 0, st>>>(a);
+      else r->interleaved ? rotary_kernel<TI, TO, true, 1><<<grid, ROT_THREADS, 0, st>>>(a) : rotary_kernel<TI, TO, false, 1><<<grid, ROT_THREADS, 0, st>>>(a);
+    });
+  });
+  return launched("spec_rotary");
+}
+
+int spec_cache_store(const spec_cache* c, const spec_store_args* r, void* cuda_stream) {
+  if (const char* why = cache_fault(c)) return fail(SPEC_E_BADARG, "spec_cache_store: %s", why);
+  if (!r) return fail(SPEC_E_BADARG, "spec_cache_store: null argument");
+  if (r->rows == 0 || r->batch == 0 || r->layers == 0 || r->max_count == 0) return SPEC_OK;
+  if (!r->k || !r->v || !r->counts) return fail(SPEC_E_BADARG, "spec_cache_store: null pointer");
+  if (r->rows < 0 || r->batch < 0 || r->layers < 0 || r->max_count < 0 || r->layer0 < 0 || r->layer0 + r->layers > c->n_layers || (!r->row_offsets && r->rows % r->batch))
+    return fail(SPEC_E_BADARG, "spec_cache_store: unsupported sizes (%d rows, batch %d, layers %d..%d of %d)", r->rows, r->batch, r->layer0, r->layer0 + r->layers, c->n_layers);
+  if (!known_type(r->type)) return fail(SPEC_E_BADARG, "spec_cache_store: unknown type");
+  const int vec = 16 / elem_size(r->type);
+  if (!aligned(r->k, 16) || !aligned(r->v, 16) || r->k_row_stride % vec || r->k_head_stride % vec || r->k_layer_stride % vec || r->v_row_stride % vec || r->v_head_stride % vec || r->v_layer_stride % vec)
+    return fail(SPEC_E_BADARG, "spec_cache_store: rows must start on 16-byte boundaries");
+  StoreArgs a{view(c), r->k, r->v, r->k_layer_stride, r->k_row_stride, r->k_head_stride, r->v_layer_stride, r->v_row_stride, r->v_head_stride, r->seqs, r->row_offsets, r->counts, r->path,
+              r->rows, r->batch, r->layer0, r->max_count, (r->max_count + CACHE_PAGE - 2) / CACHE_PAGE + 1};
+  if ((long long)a.slots * r->batch > 0x7fffffffLL || r->layers > 65535) return fail(SPEC_E_BADARG, "spec_cache_store: batch too large");
+  const dim3 grid(a.slots * r->batch, (2 * c->n_kv_heads + STORE_WARPS - 1) / STORE_WARPS, r->layers);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  by_shape(c, [&](auto d, auto f) {
+    by_type(r->type, [&](auto t) { cache_store_kernel<decltype(t), decltype(d)::value, decltype(f)::value><<<grid, 32 * STORE_WARPS, 0, st>>>(a); });
+  });
+  return launched("spec_cache_store");
+}
+
+int spec_cache_read(const spec_cache* c, const spec_read_args* r, void* cuda_stream) {
+  if (const char* why = cache_fault(c)) return fail(SPEC_E_BADARG, "spec_cache_read: %s", why);
+  if (!r) return fail(SPEC_E_BADARG, "spec_cache_read: null argument");
+  if (r->batch == 0 || r->layers == 0 || r->window == 0) return SPEC_OK;
+  if (!r->k || !r->v) return fail(SPEC_E_BADARG, "spec_cache_read: null pointer");
+  if (r->batch < 0 || r->layers < 0 || r->window < 0 || r->layer0 < 0 || r->layer0 + r->layers > c->n_layers)
+    return fail(SPEC_E_BADARG, "spec_cache_read: unsupported sizes (batch %d, window %d, layers %d..%d of %d)", r->batch, r->window, r->layer0, r->layer0 + r->layers, c->n_layers);
+  if (!known_type(r->type)) return fail(SPEC_E_BADARG, "spec_cache_read: unknown type");
+  if (!aligned(r->k, 16) || !aligned(r->v, 16)) return fail(SPEC_E_BADARG, "spec_cache_read: outputs must be 16-byte aligned");
+  ReadArgs a{view(c), r->k, r->v, r->seqs, r->start, r->batch, r->window, r->layer0, (r->window + CACHE_PAGE - 2) / CACHE_PAGE + 1};
+  if ((long long)a.slots * r->batch > 0x7fffffffLL || r->layers > 65535) return fail(SPEC_E_BADARG, "spec_cache_read: batch too large");
+  const dim3 grid(a.slots * r->batch, (2 * c->n_kv_heads + STORE_WARPS - 1) / STORE_WARPS, r->layers);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  by_shape(c, [&](auto d, auto f) {
+    by_type(r->type, [&](auto t) { cache_read_kernel<decltype(t), decltype(d)::value, decltype(f)::value><<<grid, 32 * STORE_WARPS, 0, st>>>(a); });
+  });
+  return launched("spec_cache_read");
+}
+
+size_t spec_cache_scratch_bytes(const spec_cache* c) {
+  if (cache_fault(c)) return 0;
+  return sizeof(int) * (3 * (size_t)c->n_pages + 2 * PAGES_MAX_BATCH + 4);
+}
+
+int spec_cache_fork(const spec_cache* c, int32_t batch, const int32_t* src, const int32_t* dst, void* cuda_stream) {
+  if (const char* why = cache_fault(c)) return fail(SPEC_E_BADARG, "spec_cache_fork: %s", why);
+  if (batch == 0) return SPEC_OK;
+  if (batch < 0 || !src || !dst) return fail(SPEC_E_BADARG, "spec_cache_fork: null pointer or negative batch");
+  cache_fork_kernel<<<batch, 128, 0, static_cast<cudaStream_t>(cuda_stream)>>>(view(c), src, dst);
+  return launched("spec_cache_fork");
+}
+
+int spec_cache_truncate(const spec_cache* c, int32_t batch, const int32_t* seqs, const int32_t* keep, void* cuda_stream) {
+  if (const char* why = cache_fault(c)) return fail(SPEC_E_BADARG, "spec_cache_truncate: %s", why);
+  if (batch == 0) return SPEC_OK;
+  if (batch < 0) return fail(SPEC_E_BADARG, "spec_cache_truncate: negative batch");
+  cache_truncate_kernel<<<batch, 128, 0, static_cast<cudaStream_t>(cuda_stream)>>>(view(c), seqs, keep);
+  return launched("spec_cache_truncate");
+}
+
+namespace {
+unsigned copy_blocks(size_t units) {
+  const size_t blocks = (units + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32), most = 148 * 8;
+  return (unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most);
+}
+}  // namespace
+
+int spec_cache_reserve(const spec_cache* c, int32_t batch, const int32_t* seqs, const int32_t* counts, int32_t* granted, void* scratch, size_t scratch_bytes, void* cuda_stream) {
+  if (const char* why = cache_fault(c)) return fail(SPEC_E_BADARG, "spec_cache_reserve: %s", why);
+  if (batch == 0) return SPEC_OK;
+  if (batch < 0 || batch > PAGES_MAX_BATCH || !counts || !granted) return fail(SPEC_E_BADARG, "spec_cache_reserve: null pointer or batch outside 1..%d", PAGES_MAX_BATCH);
+  if (!scratch || !aligned(scratch, 16) || scratch_bytes < spec_cache_scratch_bytes(c)) return fail(SPEC_E_NOMEM, "spec_cache_reserve: scratch of %zu bytes, 16-byte aligned, is needed", spec_cache_scratch_bytes(c));
+  int2* copies = static_cast<int2*>(scratch);
+  int* list = reinterpret_cast<int*>(copies + PAGES_MAX_BATCH);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  cache_reserve_kernel<<<1, PAGES_THREADS, 0, st>>>(view(c), seqs, counts, batch, granted, list, copies);
+  if (int rc = launched("spec_cache_reserve")) return rc;
+  cache_copy_kernel<<<copy_blocks((size_t)batch * c->n_layers * c->n_kv_heads), COPY_THREADS, 0, st>>>(view(c), copies, nullptr, batch, nullptr);
+  return launched("spec_cache_reserve: copies");
+}
+
+int spec_cache_compact(const spec_cache* c, int32_t* used, void* scratch, size_t scratch_bytes, void* cuda_stream) {
+  if (const char* why = cache_fault(c)) return fail(SPEC_E_BADARG, "spec_cache_compact: %s", why);
+  if (!used) return fail(SPEC_E_BADARG, "spec_cache_compact: null pointer");
+  if (!scratch || !aligned(scratch, 16) || scratch_bytes < spec_cache_scratch_bytes(c)) return fail(SPEC_E_NOMEM, "spec_cache_compact: scratch of %zu bytes, 16-byte aligned, is needed", spec_cache_scratch_bytes(c));
+  int2* moves = static_cast<int2*>(scratch);
+  int* to_page = reinterpret_cast<int*>(moves + c->n_pages);
+  int* n_moves = to_page + c->n_pages;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  cache_compact_kernel<<<1, PAGES_THREADS, 0, st>>>(view(c), moves, to_page, n_moves, used);
+  if (int rc = launched("spec_cache_compact")) return rc;
+  cache_copy_kernel<<<148 * 8, COPY_THREADS, 0, st>>>(view(c), moves, n_moves, 0, to_page);
+  return launched("spec_cache_compact: copies");
+}
+
+size_t spec_cache_attention_scratch(const spec_cache* c, int32_t n_heads, int32_t batch, int32_t max_rows) {
+  if (cache_fault(c) || n_heads < 1 || n_heads % c->n_kv_heads || batch < 1 || max_rows < 1) return 0;
+  return 16;
+}
+
+int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void* scratch, size_t scratch_bytes, void* cuda_stream) {
+  if (const char* why = cache_fault(c)) return fail(SPEC_E_BADARG, "spec_cache_attention: %s", why);
+  if (!r) return fail(SPEC_E_BADARG, "spec_cache_attention: null argument");
+  if (r->rows == 0 || r->batch == 0) return SPEC_OK;
+  if (!r->q || !r->k || !r->v || !r->out) return fail(SPEC_E_BADARG, "spec_cache_attention: null pointer");
+  if (r->rows < 0 || r->batch < 0 || r->batch > 65535 || r->n_heads < 1 || r->n_heads % c->n_kv_heads || r->layer < 0 || r->layer >= c->n_layers || (!r->row_offsets && r->rows % r->batch) || r->max_rows < 1 ||
+      (!r->row_offsets && r->max_rows < r->rows / r->batch) || r->mask_words < 0 || (r->mask && r->mask_words < 1))
+    return fail(SPEC_E_BADARG, "spec_cache_attention: unsupported sizes (%d rows, batch %d, %d heads over %d, layer %d of %d, max_rows %d)", r->rows, r->batch, r->n_heads, c->n_kv_heads, r->layer, c->n_layers, r->max_rows);
+  if (!known_type(r->type)) return fail(SPEC_E_BADARG, "spec_cache_attention: unknown type");
+  CacheAttnArgs a{view(c), r->q, r->k, r->v, r->q_row_stride, r->q_head_stride, r->k_row_stride, r->k_head_stride, r->v_row_stride, r->v_head_stride, r->out, r->lse, r->seqs, r->row_offsets,
+                  r->mask, r->mask_words, r->rows, r->batch, r->n_heads, r->layer, r->max_rows, r->scale};
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int per = 1024;     // rows of a sequence along x
+  const dim3 grid((unsigned)(r->n_heads * (r->max_rows < per ? r->max_rows : per)), (r->max_rows + per - 1) / per, r->batch);
+  by_shape(c, [&](auto d, auto f) {
+    by_type(r->type, [&](auto t) { cache_attention_simple<decltype(t), decltype(d)::value, decltype(f)::value><<<grid, CAS_THREADS, 0, st>>>(a); });
+  });
+  return launched("spec_cache_attention");
+}
+
+}  // extern "C"

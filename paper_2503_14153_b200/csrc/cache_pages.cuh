@@ -1,0 +1,240 @@
+// Management of the 8-bit cache's pages on the device: a page belongs to as many sequences as its reference count says; a free one has
+// count 0. Everything is decided by the counts, the tables and the lengths in device memory, so nothing waits for the host; new pages are the
+// lowest free ones, handed out in the order of the call's sequences, so that a run can be repeated number for number.
+#pragma once
+#include "cache_common.cuh"
+
+namespace spec {
+
+constexpr int PAGES_THREADS = 1024;
+constexpr int PAGES_MAX_BATCH = PAGES_THREADS;   // sequences of one call
+constexpr int PAGES_EACH = 4;                    // reference counts a thread looks at in one round
+
+// Exclusive prefix sum over the block; `total` gets the sum. All threads of the block take part.
+__device__ __forceinline__ int block_scan(int v, int* total) {
+  __shared__ int part[32];
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 31) part[w] = x;
+  __syncthreads();
+  if (w == 0) {
+    int y = lane < warps ? part[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int z = __shfl_up_sync(0xffffffffu, y, o);
+      if (lane >= o) y += z;
+    }
+    part[lane] = y;
+  }
+  __syncthreads();
+  const int before = (w ? part[w - 1] : 0) + x - v;
+  *total = part[warps - 1];
+  __syncthreads();
+  return before;
+}
+
+// ------------------------------------------------------------------ fork, truncate: a block a sequence
+__global__ void cache_fork_kernel(CacheView c, const int* __restrict__ src, const int* __restrict__ dst) {
+  const int b = blockIdx.x, s = c.sequence(src, b), d = c.sequence(dst, b);
+  if (s < 0 || d < 0) return;
+  if (s == d || c.lens[d] != 0) {
+    if (threadIdx.x == 0) set_status(c.status, ST_BOUNDS, 204, d);
+    return;
+  }
+  const int n = c.len(s), pages = (n + CACHE_PAGE - 1) / CACHE_PAGE;
+  for (int i = threadIdx.x; i < pages; i += blockDim.x) {
+    const int p = c.page(s, i);
+    c.page_table[(size_t)d * c.pages_per_seq + i] = p;
+    if (p >= 0) atomicAdd(c.refs + p, 1);
+  }
+  __syncthreads();                       // (all threads have read lens[d])
+  if (threadIdx.x == 0) c.lens[d] = n;
+}
+
+__global__ void cache_truncate_kernel(CacheView c, const int* __restrict__ seqs, const int* __restrict__ keep) {
+  const int b = blockIdx.x, s = c.sequence(seqs, b);
+  if (s < 0) return;
+  const int n = c.len(s), m = keep ? max(0, keep[b]) : 0;
+  if (m >= n) return;
+  const int from = (m + CACHE_PAGE - 1) / CACHE_PAGE, to = (n + CACHE_PAGE - 1) / CACHE_PAGE;
+  for (int i = from + threadIdx.x; i < to; i += blockDim.x) {
+    const int p = c.page(s, i);
+    if (p >= 0) atomicSub(c.refs + p, 1);
+    c.page_table[(size_t)s * c.pages_per_seq + i] = -1;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) c.lens[s] = m;
+}
+
+// ------------------------------------------------------------------ reserve
+// Room for counts[b] more tokens of every sequence: new pages, and a page of its own where the last one is partial and shared (the copy is the next
+// kernel's: `copies` [batch] gets (from, to) or (-1, -1)). A sequence gets all it needs (granted[b] = counts[b]) or nothing (0). What is shared is
+// decided before anything changes: sequences that share a page all leave it in the same call, and it is not handed out again before the next one.
+// One block: a prefix sum over the sequences' needs, a scan over the reference counts that stops when it has found enough.
+__global__ void __launch_bounds__(PAGES_THREADS)
+cache_reserve_kernel(CacheView c, const int* __restrict__ seqs, const int* __restrict__ counts, int batch, int* granted, int* list, int2* copies) {
+  __shared__ int s_seq[PAGES_MAX_BATCH], s_at[PAGES_MAX_BATCH], s_need[PAGES_MAX_BATCH], s_page[PAGES_MAX_BATCH], s_cow[PAGES_MAX_BATCH];
+  const int b = threadIdx.x;
+  int s = -1, n = 0, count = 0, held = 0, need = 0, old = -1;
+  if (b < batch) {
+    s = c.sequence(seqs, b);
+    if (s >= 0) {
+      n = c.len(s);
+      count = max(0, counts[b]);
+      held = (n + CACHE_PAGE - 1) / CACHE_PAGE;
+      if (count > c.pages_per_seq * CACHE_PAGE - n) count = 0;
+      if (count > 0) {
+        need = (n + count + CACHE_PAGE - 1) / CACHE_PAGE - held;
+        if (n % CACHE_PAGE) {
+          old = c.page(s, held - 1);
+          if (old < 0) { count = 0; need = 0; }
+          else if (c.refs[old] > 1) ++need;
+          else old = -1;
+        }
+      }
+    }
+  }
+  int total;
+  const int at = block_scan(need, &total);
+  // the lowest `total` free pages
+  int found = 0;
+  for (int base = 0; base < c.n_pages && found < total; base += PAGES_THREADS * PAGES_EACH) {
+    int mine = 0;
+    bool free[PAGES_EACH];
+#pragma unroll
+    for (int i = 0; i < PAGES_EACH; ++i) {
+      const int p = base + threadIdx.x * PAGES_EACH + i;
+      free[i] = p < c.n_pages && c.refs[p] == 0;
+      mine += free[i];
+    }
+    int here;
+    int r = found + block_scan(mine, &here);
+#pragma unroll
+    for (int i = 0; i < PAGES_EACH; ++i)
+      if (free[i]) {
+        if (r < total) list[r] = base + threadIdx.x * PAGES_EACH + i;
+        ++r;
+      }
+    found += here;
+  }
+  const bool ok = at + need <= found;
+  if (b < batch) {
+    s_seq[b] = s;
+    s_at[b] = at;
+    s_need[b] = ok ? need : 0;
+    s_page[b] = held;
+    s_cow[b] = old >= 0;
+  }
+  __syncthreads();                       // (the list, too, is seen by all threads of the block)
+  for (int e = threadIdx.x >> 5; e < batch; e += PAGES_THREADS / 32) {
+    const int cow = s_cow[e];
+    for (int i = threadIdx.x & 31; i < s_need[e]; i += 32) {
+      const int p = list[s_at[e] + i];
+      c.page_table[(size_t)s_seq[e] * c.pages_per_seq + s_page[e] + i - cow] = p;
+      c.refs[p] = 1;
+    }
+  }
+  if (b < batch) {
+    int2 copy = make_int2(-1, -1);
+    if (ok && old >= 0) {
+      copy = make_int2(old, list[at]);
+      atomicSub(c.refs + old, 1);
+    }
+    copies[b] = copy;
+    if (!ok) count = 0;
+    granted[b] = count;
+    if (s >= 0 && count > 0) c.lens[s] = n + count;
+  }
+}
+
+// ------------------------------------------------------------------ compact
+// The pages in use move to the numbers below their count: the i-th used page at or above it goes to the i-th free one below.
+// moves[i] = (from, to); to_page[p] = where page p is now; *n_moves, *used.
+__global__ void __launch_bounds__(PAGES_THREADS) cache_compact_kernel(CacheView c, int2* moves, int* to_page, int* n_moves, int* used) {
+  int mine = 0;
+  for (int p = threadIdx.x; p < c.n_pages; p += PAGES_THREADS) {
+    mine += c.refs[p] > 0;
+    to_page[p] = p;
+  }
+  int in_use;
+  block_scan(mine, &in_use);
+  int holes = 0, movers = 0;
+  for (int base = 0; base < c.n_pages; base += PAGES_THREADS * PAGES_EACH) {
+    bool hole[PAGES_EACH], mover[PAGES_EACH];
+    int nh = 0, nm = 0;
+#pragma unroll
+    for (int i = 0; i < PAGES_EACH; ++i) {
+      const int p = base + threadIdx.x * PAGES_EACH + i;
+      const bool held = p < c.n_pages && c.refs[p] > 0;
+      hole[i] = p < in_use && !held;
+      mover[i] = p >= in_use && held;
+      nh += hole[i];
+      nm += mover[i];
+    }
+    int th, tm;
+    int rh = holes + block_scan(nh, &th), rm = movers + block_scan(nm, &tm);
+#pragma unroll
+    for (int i = 0; i < PAGES_EACH; ++i) {
+      const int p = base + threadIdx.x * PAGES_EACH + i;
+      if (hole[i]) moves[rh++].y = p;
+      if (mover[i]) moves[rm++].x = p;
+    }
+    holes += th;
+    movers += tm;
+  }
+  __syncthreads();                       // (there are as many holes as movers)
+  for (int i = threadIdx.x; i < movers; i += PAGES_THREADS) {
+    const int2 m = moves[i];
+    to_page[m.x] = m.y;
+    c.refs[m.y] = c.refs[m.x];
+    c.refs[m.x] = 0;
+  }
+  if (threadIdx.x == 0) {
+    *n_moves = movers;
+    *used = in_use;
+  }
+}
+
+// ------------------------------------------------------------------ copies of pages
+// The blocks of every (layer, head) of each listed page, K and V together: 2 * 16 * D bytes and two scales, a warp a copy. Source pages keep what they
+// hold; no page is both source and target of one call. With `to_page` the page tables are renumbered, too.
+constexpr int COPY_THREADS = 256;
+__global__ void __launch_bounds__(COPY_THREADS)
+cache_copy_kernel(CacheView c, const int2* __restrict__ list, const int* __restrict__ count, int fixed_count, const int* __restrict__ to_page) {
+  const int n = count ? *count : fixed_count;
+  const int lane = threadIdx.x & 31;
+  const size_t pairs = (size_t)c.n_layers * c.kv, units = pairs * n;
+  const int vecs = 2 * CACHE_PAGE * c.D / 16;
+  const size_t warp0 = ((size_t)blockIdx.x * COPY_THREADS + threadIdx.x) >> 5, warps = (size_t)gridDim.x * (COPY_THREADS / 32);
+  for (size_t u = warp0; u < units; u += warps) {
+    const int2 m = list[u / pairs];
+    if (m.x < 0 || m.y < 0 || m.x >= c.n_pages || m.y >= c.n_pages) continue;
+    const size_t first = (u % pairs) * c.n_pages;
+    const uint4* from = reinterpret_cast<const uint4*>(c.codes + (first + m.x) * (2 * (size_t)CACHE_PAGE * c.D));
+    uint4* to = reinterpret_cast<uint4*>(c.codes + (first + m.y) * (2 * (size_t)CACHE_PAGE * c.D));
+    for (int i = lane; i < vecs; i += 128) {
+      uint4 x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + 32 * j < vecs) x[j] = from[i + 32 * j];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + 32 * j < vecs) to[i + 32 * j] = x[j];
+    }
+    if (lane < 2) c.scales[(first + m.y) * 2 + lane] = c.scales[(first + m.x) * 2 + lane];
+  }
+  if (to_page) {
+    const size_t entries = (size_t)c.max_seqs * c.pages_per_seq;
+    for (size_t i = (size_t)blockIdx.x * COPY_THREADS + threadIdx.x; i < entries; i += (size_t)gridDim.x * COPY_THREADS) {
+      const int p = c.page_table[i];
+      if (p >= 0 && p < c.n_pages) c.page_table[i] = to_page[p];
+    }
+  }
+}
+
+}  // namespace spec

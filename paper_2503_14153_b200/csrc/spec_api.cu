@@ -2079,6 +2079,16 @@ int step_t(spec_ctx* c, int32_t* out_tokens, int32_t* out_counts, const int32_t*
 
 }  // namespace
 
+// Text of a failed call that has no context, for the library's other source files.
+namespace spec {
+void set_last_error(const char* text) noexcept {
+  try {
+    g_create_error = text;
+  } catch (...) {
+  }
+}
+}  // namespace spec
+
 extern "C" {
 
 size_t spec_workspace_bytes(const spec_config* cfg, const spec_tree* tree) {
