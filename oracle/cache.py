@@ -1,0 +1,167 @@
+"""Plain definition of the 8-bit paged cache, attention over it and rotary positions, in 64 bits.
+
+A page holds 16 tokens; per (layer, kv head, page) K and V have one scale each and a code for every value: an integer in
+-127..127, or one of the e4m3 numbers. Here codes are kept as the numbers they stand for, [token][dim], in no storage order.
+"""
+import numpy as np
+
+PAGE = 16
+CODE_MAX = {"int8": 127.0, "e4m3": 448.0}
+
+
+def e4m3_values():
+    """The 127 non-negative finite e4m3 numbers, ascending (code 0x7f is NaN)."""
+    out = []
+    for code in range(127):
+        e, m = code >> 3, code & 7
+        out.append((1 + m / 8) * 2.0 ** (e - 7) if e else m / 8 * 2.0 ** -6)
+    return np.array(out)
+
+
+_E4M3 = e4m3_values()
+
+
+def nearest_code(x, fmt):
+    """x (in units of the scale) to the nearest code, ties to the even one, held inside the range; NaN to 0."""
+    x = np.where(np.isnan(x), 0.0, np.asarray(x, dtype=np.float64))
+    if fmt == "int8":
+        return np.clip(np.rint(np.clip(x, -1e6, 1e6)), -127, 127)
+    a = np.minimum(np.abs(x), 448.0)
+    hi = np.clip(np.searchsorted(_E4M3, a), 1, 126)
+    lo = hi - 1
+    below, above = a - _E4M3[lo], _E4M3[hi] - a
+    pick = np.where(below < above, lo, np.where(above < below, hi, np.where(lo % 2 == 0, lo, hi)))
+    return np.copysign(_E4M3[pick], x)
+
+
+def block_scale(rows, before, fmt):
+    """Scale of a block that takes `rows`; `before`: the scale it had if it held tokens, else 0."""
+    a = np.abs(rows)
+    top = np.max(np.where(np.isfinite(a), a, 0.0), initial=0.0)
+    return max(before, 0.0 if top < 2.0 ** -100 else top / CODE_MAX[fmt])
+
+
+class Cache:
+    def __init__(self, layers, kv, D, n_pages, max_seqs, pages_per_seq, fmt):
+        self.codes = np.zeros((layers, kv, n_pages, 2, PAGE, D))
+        self.scales = np.zeros((layers, kv, n_pages, 2))
+        self.table = -np.ones((max_seqs, pages_per_seq), dtype=np.int64)
+        self.refs = np.zeros(n_pages, dtype=np.int64)
+        self.lens = np.zeros(max_seqs, dtype=np.int64)
+        self.fmt = fmt
+
+    # ---- pages
+    def fork(self, src, dst):
+        for s, d in zip(src, dst):
+            for i in range(-(-int(self.lens[s]) // PAGE)):
+                self.table[d, i] = self.table[s, i]
+                self.refs[self.table[s, i]] += 1
+            self.lens[d] = self.lens[s]
+
+    def truncate(self, seqs, keep):
+        for s, m in zip(seqs, keep):
+            if m >= self.lens[s]:
+                continue
+            for i in range(-(-m // PAGE), -(-int(self.lens[s]) // PAGE)):
+                self.refs[self.table[s, i]] -= 1
+                self.table[s, i] = -1
+            self.lens[s] = m
+
+    def reserve(self, seqs, counts):
+        shared = self.refs > 1                                  # as the call found it
+        free = [p for p in range(len(self.refs)) if self.refs[p] == 0]
+        granted, asked = [], 0
+        for s, c in zip(seqs, counts):
+            n = int(self.lens[s])
+            held, want = -(-n // PAGE), -(-(n + c) // PAGE)
+            if c <= 0 or want > self.table.shape[1]:
+                granted.append(0)
+                continue
+            copy = n % PAGE != 0 and shared[self.table[s, held - 1]]
+            asked += want - held + copy                         # (what a sequence asks for counts for the next ones, granted or not)
+            if asked > len(free):
+                granted.append(0)
+                continue
+            mine = free[asked - (want - held + copy):asked]
+            if copy:
+                old, new = self.table[s, held - 1], mine.pop(0)
+                self.codes[:, :, new], self.scales[:, :, new] = self.codes[:, :, old], self.scales[:, :, old]
+                self.refs[old] -= 1
+                self.refs[new] = 1
+                self.table[s, held - 1] = new
+            for i, p in enumerate(mine):
+                self.table[s, held + i] = p
+                self.refs[p] = 1
+            self.lens[s] = n + c
+            granted.append(c)
+        return granted
+
+    def compact(self):
+        used = int((self.refs > 0).sum())
+        movers = [p for p in range(used, len(self.refs)) if self.refs[p] > 0]
+        holes = [p for p in range(used) if self.refs[p] == 0]
+        for a, b in zip(movers, holes):
+            self.codes[:, :, b], self.scales[:, :, b] = self.codes[:, :, a], self.scales[:, :, a]
+            self.refs[b], self.refs[a] = self.refs[a], 0
+            self.table[self.table == a] = b
+        return used
+
+    # ---- rows
+    def store(self, seq, rows, layer0=0):
+        """rows [layers][K|V][count][kv][D] are the last `count` tokens of the sequence."""
+        layers, _, count, kv, _ = rows.shape
+        end = int(self.lens[seq])
+        first = end - count
+        for p in range(first // PAGE, -(-end // PAGE)) if count else ():
+            page = self.table[seq, p]
+            lo, hi = max(first, p * PAGE), min(end, (p + 1) * PAGE)
+            for l in range(layers):
+                for h in range(kv):
+                    for w in range(2):
+                        new, at = rows[l, w, lo - first:hi - first, h], (layer0 + l, h, page, w)
+                        before = self.scales[at] if lo > p * PAGE else 0.0
+                        now = block_scale(new, before, self.fmt)
+                        old = self.codes[at][:lo - p * PAGE] * before
+                        both = np.concatenate([old, new])
+                        self.codes[at] = 0.0
+                        if now > 0:
+                            self.codes[at][:hi - p * PAGE] = nearest_code(both / now, self.fmt)
+                        self.scales[at] = now
+
+    def rows(self, seq, layer, which):
+        """All tokens of a sequence [len][kv][D]."""
+        n = int(self.lens[seq])
+        pages = self.table[seq, :-(-n // PAGE)]
+        x = self.codes[layer][:, pages, which] * self.scales[layer][:, pages, which][..., None, None]
+        return x.reshape(x.shape[0], -1, x.shape[-1])[:, :n].transpose(1, 0, 2)
+
+
+def attention(q, k, v, cached_k, cached_v, sees, scale):
+    """q [R][H][D]; k, v [R][kv][D]; cached [n][kv][D]; sees [R][R] bool. Returns (out, lse, sum of weight * |v| for error bounds)."""
+    R, H, D = q.shape
+    n, kv = cached_k.shape[:2]
+    out, lse, mass = np.zeros((R, H, D)), np.full((R, H), -np.inf), np.zeros((R, H, D))
+    for h in range(H):
+        g = h // (H // kv)
+        for i in range(R):
+            mine = np.flatnonzero(sees[i])
+            K = np.concatenate([cached_k[:, g], k[mine, g]])
+            V = np.concatenate([cached_v[:, g], v[mine, g]])
+            if not len(K):
+                continue
+            z = scale * (K @ q[i, h])
+            top = z.max()
+            w = np.exp(z - top)
+            out[i, h], lse[i, h], mass[i, h] = w @ V / w.sum(), top + np.log(w.sum()), w @ np.abs(V) / w.sum()
+    return out, lse, mass
+
+
+def rotate(x, positions, freq, gain, interleaved):
+    """The first 2 * len(freq) values of each head [rows][heads][D] turn in pairs."""
+    rot = 2 * len(freq)
+    a = np.asarray(positions, dtype=np.float64)[:, None, None] * np.asarray(freq)
+    c, s = gain * np.cos(a), gain * np.sin(a)
+    lo, hi = (slice(0, rot, 2), slice(1, rot, 2)) if interleaved else (slice(0, rot // 2), slice(rot // 2, rot))
+    y = np.array(x, dtype=np.float64)
+    y[..., lo], y[..., hi] = x[..., lo] * c - x[..., hi] * s, x[..., hi] * c + x[..., lo] * s
+    return y

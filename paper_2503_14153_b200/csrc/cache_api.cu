@@ -40,7 +40,7 @@ const char* cache_fault(const spec_cache* c) {
   if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
   if (c->format != SPEC_CACHE_INT8 && c->format != SPEC_CACHE_E4M3) return "format must be SPEC_CACHE_INT8 or SPEC_CACHE_E4M3";
   if (c->n_pages > (1 << 27) || c->pages_per_seq > (1 << 26)) return "cache too large (2^27 pages, 2^30 tokens a sequence)";
-  if (!aligned(c->codes, 16)) return "codes must be 16-byte aligned";
+  if (!aligned(c->codes, 16) || !aligned(c->scales, 8)) return "codes must be 16-byte aligned, scales 8-byte";
   return nullptr;
 }
 
@@ -63,6 +63,35 @@ template <typename F> auto by_shape(const spec_cache* c, F f) {
   return c->format == SPEC_CACHE_INT8 ? f(Int<64>{}, Int<CACHE_INT8>{}) : f(Int<64>{}, Int<CACHE_E4M3>{});
 }
 
+// Row groups of 16 (sequence row, head) rows that a CTA of the tensor-core kernel has: as few as hold all rows of a (sequence, kv head), at most 4.
+int row_groups(long long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+struct AttnShape {
+  int rg, mt;
+  long long tiles, pairs;       // row tiles of a sequence, (sequence, row tile) pairs of a launch at most
+  size_t arrive_bytes, bytes;
+};
+AttnShape attn_shape(const spec_cache* c, int n_heads, int batch, int max_rows) {
+  AttnShape s;
+  const long long rows = (long long)max_rows * (n_heads / c->n_kv_heads);
+  s.rg = row_groups(rows);
+  s.mt = 16 * s.rg;
+  s.tiles = (rows + s.mt - 1) / s.mt;
+  s.pairs = s.tiles * batch < CAM_PAIRS ? s.tiles * batch : CAM_PAIRS;
+  s.arrive_bytes = ((size_t)s.pairs * c->n_kv_heads * 4 + 255) / 256 * 256;
+  s.bytes = s.arrive_bytes + (size_t)2 * CAM_SMS * 2 * s.mt * (c->head_dim + 2) * 4;
+  return s;
+}
+template <typename T, int D, int FMT, int RG> int launch_mma(const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
+  auto kernel = cache_attention_mma<T, D, FMT, RG>;
+  const size_t smem = cam_smem(D, RG);
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return launched("spec_cache_attention: shared memory");
+  kernel<<<CAM_SMS * (RG == 4 ? 1 : 2), CAM_THREADS, smem, st>>>(a, pl);
+  return launched("spec_cache_attention");
+}
+unsigned copy_blocks(size_t units) {
+  const size_t blocks = (units + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32), most = 148 * 8;
+  return (unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most);
+}
 }  // namespace
 
 extern "C" {
@@ -170,13 +199,6 @@ int spec_cache_truncate(const spec_cache* c, int32_t batch, const int32_t* seqs,
   return launched("spec_cache_truncate");
 }
 
-namespace {
-unsigned copy_blocks(size_t units) {
-  const size_t blocks = (units + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32), most = 148 * 8;
-  return (unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most);
-}
-}  // namespace
-
 int spec_cache_reserve(const spec_cache* c, int32_t batch, const int32_t* seqs, const int32_t* counts, int32_t* granted, void* scratch, size_t scratch_bytes, void* cuda_stream) {
   if (const char* why = cache_fault(c)) return fail(SPEC_E_BADARG, "spec_cache_reserve: %s", why);
   if (batch == 0) return SPEC_OK;
@@ -207,7 +229,7 @@ int spec_cache_compact(const spec_cache* c, int32_t* used, void* scratch, size_t
 
 size_t spec_cache_attention_scratch(const spec_cache* c, int32_t n_heads, int32_t batch, int32_t max_rows) {
   if (cache_fault(c) || n_heads < 1 || n_heads % c->n_kv_heads || batch < 1 || max_rows < 1) return 0;
-  return 16;
+  return attn_shape(c, n_heads, batch, max_rows).bytes;
 }
 
 int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void* scratch, size_t scratch_bytes, void* cuda_stream) {
@@ -216,18 +238,43 @@ int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void
   if (r->rows == 0 || r->batch == 0) return SPEC_OK;
   if (!r->q || !r->k || !r->v || !r->out) return fail(SPEC_E_BADARG, "spec_cache_attention: null pointer");
   if (r->rows < 0 || r->batch < 0 || r->batch > 65535 || r->n_heads < 1 || r->n_heads % c->n_kv_heads || r->layer < 0 || r->layer >= c->n_layers || (!r->row_offsets && r->rows % r->batch) || r->max_rows < 1 ||
-      (!r->row_offsets && r->max_rows < r->rows / r->batch) || r->mask_words < 0 || (r->mask && r->mask_words < 1))
+      (!r->row_offsets && r->max_rows < r->rows / r->batch) || r->mask_words < 0 || (r->mask && r->mask_words < 1) || (long long)r->rows * r->n_heads > 0x7fffffffLL)
     return fail(SPEC_E_BADARG, "spec_cache_attention: unsupported sizes (%d rows, batch %d, %d heads over %d, layer %d of %d, max_rows %d)", r->rows, r->batch, r->n_heads, c->n_kv_heads, r->layer, c->n_layers, r->max_rows);
   if (!known_type(r->type)) return fail(SPEC_E_BADARG, "spec_cache_attention: unknown type");
+  if (r->type != SPEC_TYPE_F32) {
+    if (!aligned(r->q, 16) || !aligned(r->k, 16) || !aligned(r->v, 16) || !aligned(r->out, 16) || r->q_row_stride % 8 || r->q_head_stride % 8 || r->k_row_stride % 8 || r->k_head_stride % 8 || r->v_row_stride % 8 || r->v_head_stride % 8)
+      return fail(SPEC_E_BADARG, "spec_cache_attention: rows must start on 16-byte boundaries");
+  }
+  const int max_rows = r->max_rows < r->rows ? r->max_rows : r->rows;
+  const AttnShape sh = attn_shape(c, r->n_heads, r->batch, r->max_rows);
+  if (!scratch || !aligned(scratch, 16) || scratch_bytes < sh.bytes) return fail(SPEC_E_NOMEM, "spec_cache_attention: scratch of %zu bytes, 16-byte aligned, is needed", sh.bytes);
   CacheAttnArgs a{view(c), r->q, r->k, r->v, r->q_row_stride, r->q_head_stride, r->k_row_stride, r->k_head_stride, r->v_row_stride, r->v_head_stride, r->out, r->lse, r->seqs, r->row_offsets,
-                  r->mask, r->mask_words, r->rows, r->batch, r->n_heads, r->layer, r->max_rows, r->scale};
+                  r->mask, r->mask_words, r->rows, r->batch, r->n_heads, r->layer, max_rows, r->scale};
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int per = 1024;     // rows of a sequence along x
-  const dim3 grid((unsigned)(r->n_heads * (r->max_rows < per ? r->max_rows : per)), (r->max_rows + per - 1) / per, r->batch);
-  by_shape(c, [&](auto d, auto f) {
-    by_type(r->type, [&](auto t) { cache_attention_simple<decltype(t), decltype(d)::value, decltype(f)::value><<<grid, CAS_THREADS, 0, st>>>(a); });
-  });
-  return launched("spec_cache_attention");
+  if (r->type == SPEC_TYPE_F32) {
+    const int per = 1024;     // rows of a sequence along x
+    const dim3 grid((unsigned)(r->n_heads * (max_rows < per ? max_rows : per)), (max_rows + per - 1) / per, r->batch);
+    by_shape(c, [&](auto d, auto f) { cache_attention_simple<float, decltype(d)::value, decltype(f)::value><<<grid, CAS_THREADS, 0, st>>>(a); });
+    return launched("spec_cache_attention");
+  }
+  // launches of at most CAM_PAIRS (sequence, row tile) pairs
+  const int tiles = (int)(((long long)max_rows * (r->n_heads / c->n_kv_heads) + sh.mt - 1) / sh.mt);
+  const int nrt = tiles < CAM_PAIRS ? tiles : CAM_PAIRS, nb = CAM_PAIRS / nrt;
+  for (int b0 = 0; b0 < r->batch; b0 += nb)
+    for (int rt0 = 0; rt0 < tiles; rt0 += nrt) {
+      const CamPlan pl{b0, r->batch - b0 < nb ? r->batch - b0 : nb, rt0, tiles - rt0 < nrt ? tiles - rt0 : nrt, static_cast<int*>(scratch),
+                       reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + sh.arrive_bytes)};
+      const int rc = by_shape(c, [&](auto d, auto f) {
+        auto go = [&](auto t) {
+          typedef decltype(t) T;
+          constexpr int D = decltype(d)::value, F = decltype(f)::value;
+          return sh.rg == 1 ? launch_mma<T, D, F, 1>(a, pl, st) : sh.rg == 2 ? launch_mma<T, D, F, 2>(a, pl, st) : launch_mma<T, D, F, 4>(a, pl, st);
+        };
+        return r->type == SPEC_TYPE_BF16 ? go(bf16{}) : go(f16{});
+      });
+      if (rc) return rc;
+    }
+  return SPEC_OK;
 }
 
 }  // extern "C"

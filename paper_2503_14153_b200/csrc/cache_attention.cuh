@@ -3,6 +3,8 @@
 // j over the n cached tokens of the row's sequence (codes * scale of their page and head) and the rows of the pass that the row's mask shows (16-bit, not yet
 // in the cache). lse_i = log sum_j w_ij. A row that sees nothing gives zeros and lse -infinity.
 #pragma once
+#include <type_traits>
+
 #include "cache_common.cuh"
 #include "cache_rows.cuh"
 
@@ -119,6 +121,633 @@ __global__ void __launch_bounds__(CAS_THREADS) cache_attention_simple(CacheAttnA
   const bool none = l == 0.f;
   static_cast<T*>(a.out)[((size_t)row * a.H + h) * D + d] = from_f<T>(none ? 0.f : acc / l);
   if (a.lse && tid == 0) a.lse[(size_t)row * a.H + h] = none ? -INFINITY : (m == -INFINITY ? 0.f : m) * 0.693147180559945f + logf(l);
+}
+
+
+// ------------------------------------------------------------------ the tensor-core kernel for few rows
+// mma.sync m16n8k16 with float32 sums. A unit is (sequence, kv head, row tile): the MT = 16 RG rows of a tile are (row of the pass, query head of the kv head's group), so
+// that a group's heads share what is read. 8 warps as RG row groups x KG key groups walk the unit's tiles: 128 cached tokens (8 pages) or 64 rows of the pass, 256 D bytes
+// either way, in a ring of cp.async stages.
+//
+// Codes meet q as float16 (exact for int8 and for e4m3 / 256, both by bit tricks); a bf16 row of q is scaled by a power of two into float16's range first, which loses
+// nothing above 2^-32 of its largest value. The page's scale of K multiplies the scores. Its scale of V goes into the exponent: with z' = z + log2(sv) the weights w' = 2^(z' - max z') = w sv / const meet the codes
+// of V as they are, w' is at most 1, and the sum of the weights adds w' / sv. So pages of any scale share one accumulator. Rows of the pass count as a page of scale c, the sequence's first
+// page's, and their weights are w' / c in the operand type.
+//
+// Work: every CTA gets an equal run of consecutive tiles of the list of all units (sequence, head, row tile), which it works out from the lengths in device memory; a unit cut by the
+// end of a run leaves (max, sum, values) in scratch and the last of its CTAs to arrive adds the parts in the order of the CTAs.
+constexpr int CAM_WARPS = 8, CAM_THREADS = 32 * CAM_WARPS;
+constexpr int CAM_TILE = 128, CAM_PAGES = CAM_TILE / CACHE_PAGE, CAM_NEW = 64;   // cached tokens and rows of the pass a tile
+constexpr int CAM_PAIRS = 4096;          // (sequence, row tile) pairs a launch can deal
+constexpr int CAM_SMS = 148;
+
+struct CamPlan {
+  int b0, nb, rt0, nrt;                  // this launch: sequences b0 .. b0 + nb - 1, row tiles rt0 .. rt0 + nrt - 1
+  int* arrive;                           // [nb * nrt * kv], zero between launches
+  float* part;                           // [CTAs][2][MT][D + 2]
+};
+
+__host__ __device__ constexpr int cam_stage_bytes(int D) { return 256 * D + 128; }
+__host__ __device__ constexpr int cam_stages(int RG) { return 3; }
+__host__ __device__ constexpr size_t cam_smem(int D, int RG) { return (size_t)cam_stages(RG) * cam_stage_bytes(D); }
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void cam_ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void cam_ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <typename T> __device__ __forceinline__ void cam_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (sizeof(T) == 2 && std::is_same<T, bf16>::value)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if constexpr (std::is_same<T, bf16>::value) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  } else {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t w) {
+  if constexpr (std::is_same<T, bf16>::value) return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w));
+  else return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+// true if one of the two 16-bit values is infinite or NaN
+template <typename T> __device__ __forceinline__ bool odd2(uint32_t w) {
+  constexpr uint32_t e = std::is_same<T, bf16>::value ? 0x7f80u : 0x7c00u;
+  return (w & e) == e || ((w >> 16) & e) == e;
+}
+// the pair with infinities and NaN replaced by zero
+template <typename T> __device__ __forceinline__ uint32_t tame2(uint32_t w) {
+  constexpr uint32_t e = std::is_same<T, bf16>::value ? 0x7f80u : 0x7c00u;
+  return ((w & e) == e ? 0u : w & 0xffffu) | (((w >> 16) & e) == e ? 0u : w & 0xffff0000u);
+}
+
+// Four codes -> float16 pairs (bytes 0, 1), (bytes 2, 3): the int8 value, or the e4m3 value / 256.
+// int8: 0x6400 + (code + 128) is the float16 number 1024 + code + 128. e4m3: exponent and mantissa move into float16's fields (bias 7 against 15, so / 2^8, subnormals included); the NaN code becomes a number.
+template <int FMT> __device__ __forceinline__ void codes_to_f16(uint32_t w, uint32_t& a, uint32_t& b) {
+  if constexpr (FMT == CACHE_INT8) {
+    const uint32_t u = w ^ 0x80808080u;
+    const uint32_t magic = 0x64646464u, off = 0x64806480u;
+    const uint32_t x = __byte_perm(u, magic, 0x4140), y = __byte_perm(u, magic, 0x4342);
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(a) : "r"(x), "r"(off));
+    asm("sub.f16x2 %0, %1, %2;" : "=r"(b) : "r"(y), "r"(off));
+  } else {
+    const uint32_t x = __byte_perm(w, 0, 0x1404), y = __byte_perm(w, 0, 0x3424);
+    a = ((x >> 1) & 0x3f803f80u) | (x & 0x80008000u);
+    b = ((y >> 1) & 0x3f803f80u) | (y & 0x80008000u);
+  }
+}
+template <int FMT> __host__ __device__ constexpr float code_unit() { return FMT == CACHE_INT8 ? 1.f : 256.f; }
+// Four codes of V -> pairs of the operand type that the weights are rounded to. bf16 (8 significant bits hold any int8): 0x4300 + low 7 bits is 128 + them, 0x4300 + the sign bit 128 or 256, and
+// their difference the code; e4m3 fields move to bf16's (bias 7 against 127: times 2^120 to make it the value, divided by 256 here too).
+template <int FMT, typename T> __device__ __forceinline__ void codes_to(uint32_t w, uint32_t& a, uint32_t& b) {
+  if constexpr (!std::is_same<T, bf16>::value) {
+    codes_to_f16<FMT>(w, a, b);
+  } else if constexpr (FMT == CACHE_INT8) {
+    const uint32_t x = __byte_perm(w, 0x43434343u, 0x4140), y = __byte_perm(w, 0x43434343u, 0x4342);
+    asm("sub.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(x & 0xff7fff7fu), "r"(x & 0xff80ff80u));
+    asm("sub.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(y & 0xff7fff7fu), "r"(y & 0xff80ff80u));
+  } else {
+    const uint32_t x = __byte_perm(w, 0, 0x1404), y = __byte_perm(w, 0, 0x3424), up = 0x77807780u;   // 2^112
+    asm("mul.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(((x >> 4) & 0x07f007f0u) | (x & 0x80008000u)), "r"(up));
+    asm("mul.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(((y >> 4) & 0x07f007f0u) | (y & 0x80008000u)), "r"(up));
+  }
+}
+
+// visibility of rows 64 tile .. 64 tile + 63 of the pass to row i of the sequence (bits), `count` rows in all
+__device__ __forceinline__ unsigned long long sees64(const uint32_t* mask, int words, size_t row, int i, int tile, int count) {
+  const int k0 = tile * 64;
+  unsigned long long v;
+  if (mask) {
+    const uint32_t* m = mask + row * words + 2 * tile;
+    v = 2 * tile < words ? m[0] : 0u;
+    if (2 * tile + 1 < words) v |= (unsigned long long)m[1] << 32;
+  } else {
+    const int d = i - k0;                        // sees k0 .. i
+    v = d >= 63 ? ~0ull : d < 0 ? 0ull : (2ull << d) - 1;
+  }
+  const int left = count - k0;
+  return left >= 64 ? v : left <= 0 ? 0ull : v & ((1ull << left) - 1);
+}
+
+template <typename T, int D, int FMT, int RG>
+__global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_mma(CacheAttnArgs a, CamPlan pl) {
+  constexpr int KG = CAM_WARPS / RG, MT = 16 * RG, ST = cam_stages(RG), NP = CAM_PAGES / KG;
+  constexpr int DC = D / 16, DT = D / 8, STAGE = cam_stage_bytes(D), BLOCK = CACHE_PAGE * D;
+  constexpr bool ALONE = RG == 1;                // a warp uses only the pages it fetched itself
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int pre[CAM_PAIRS + 1];
+  __shared__ int scan[CAM_WARPS];
+  __shared__ int last;
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  const int rg = warp % RG, kg = warp / RG;
+  const int G = a.H / c.kv, pairs = pl.nb * pl.nrt;
+
+  // ---- the list of units: tiles of every (sequence, row tile), one kv head; prefix sums
+  auto rows_of = [&](int b, int& r0) {
+    r0 = rows_begin(a.row_offsets, b, a.rows, a.batch);
+    return max(0, rows_begin(a.row_offsets, b + 1, a.rows, a.batch) - r0);
+  };
+  auto tiles_of = [&](int pair, int& cached) {
+    const int b = pl.b0 + pair / pl.nrt, rt = pl.rt0 + pair % pl.nrt;
+    int r0;
+    const int R = rows_of(b, r0), left = R * G - rt * MT;
+    cached = 0;
+    if (left <= 0) return 0;
+    const int s = c.sequence(a.seqs, b);
+    cached = s < 0 ? 0 : (c.len(s) + CAM_TILE - 1) / CAM_TILE;
+    const int seen = a.mask ? R : min(R, (rt * MT + min(left, MT) - 1) / G + 1);
+    return cached + (seen + CAM_NEW - 1) / CAM_NEW;
+  };
+  {
+    const int each = (pairs + CAM_THREADS - 1) / CAM_THREADS;
+    int mine = 0, dummy;
+    for (int i = 0; i < each; ++i) {
+      const int p = tid * each + i;
+      if (p < pairs) mine += tiles_of(p, dummy);
+    }
+    int x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) scan[warp] = x;
+    __syncthreads();
+    int at = x - mine;
+    for (int w = 0; w < warp; ++w) at += scan[w];
+    for (int i = 0; i < each; ++i) {
+      const int p = tid * each + i;
+      if (p < pairs) {
+        pre[p] = at;
+        at += tiles_of(p, dummy);
+        if (p == pairs - 1) pre[pairs] = at;
+      }
+    }
+    __syncthreads();
+  }
+  const long long total = (long long)pre[pairs] * c.kv;
+  const long long ctas = min((long long)gridDim.x, total);
+  if (blockIdx.x >= ctas) return;
+  auto run_begin = [&](long long cta) { return cta * total / ctas; };
+  auto owner = [&](long long tile) { return ((tile + 1) * ctas - 1) / total; };
+  const long long run0 = run_begin(blockIdx.x), run1 = run_begin(blockIdx.x + 1ll);
+
+  for (long long at = run0; at < run1;) {
+    // ---- which unit
+    int b, kvh, rt, tile0, tiles;
+    long long unit0;
+    {
+      int lo = 0, hi = pl.nb;                    // sequence: the last one whose units begin at or before `at` and that has any
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((long long)pre[mid * pl.nrt] * c.kv <= at) lo = mid; else hi = mid;
+      }
+      b = lo;
+      const int p0 = b * pl.nrt, w = pre[p0 + pl.nrt] - pre[p0];
+      const long long in = at - (long long)pre[p0] * c.kv;
+      kvh = (int)(in / w);
+      const int r = (int)(in % w) + pre[p0];
+      lo = p0, hi = p0 + pl.nrt;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (pre[mid] <= r) lo = mid; else hi = mid;
+      }
+      rt = lo - p0;
+      tiles = pre[lo + 1] - pre[lo];
+      tile0 = r - pre[lo];
+      unit0 = at - tile0;
+    }
+    const int tile1 = (int)min((long long)tiles, tile0 + (run1 - at));
+    const int seq_b = pl.b0 + b, rtile = pl.rt0 + rt;
+    int r0, cached;
+    const int R = rows_of(seq_b, r0);
+    tiles_of(b * pl.nrt + rt, cached);
+    const int s = c.sequence(a.seqs, seq_b);
+    const int n = s < 0 ? 0 : c.len(s);
+    const size_t head_block = ((size_t)a.layer * c.kv + kvh) * c.n_pages;
+
+    // ---- fetches: one group of copies a tile
+    auto issue = [&](int tile) {
+      if (tile < tile1) {
+        uint8_t* st = smem + (tile % ST) * STAGE;
+        if (tile < cached) {
+          // a warp a page
+          const int p = tile * CAM_PAGES + warp;
+          const uint32_t dst = smem_u32(st + warp * 2 * BLOCK) + lane * 16;
+          float2* sc = reinterpret_cast<float2*>(st + 256 * D) + warp;
+          const int page = p * CACHE_PAGE < n ? c.page(s, p) : -1;
+          if (page >= 0) {
+            const uint8_t* src = c.codes + (head_block + page) * (2 * BLOCK) + lane * 16;
+#pragma unroll
+            for (int i = 0; i < 2 * BLOCK / 512; ++i) cp_async16(dst + i * 512, src + i * 512, 16);
+            if (lane == 0) cp_async8(smem_u32(sc), c.scales + (head_block + page) * 2);
+          } else if (lane == 0) {
+            *sc = make_float2(0.f, 0.f);
+          }
+        } else {
+          // 64 rows of k, then of v; 16-byte chunk ch of row r at chunk ch ^ x(r)
+          const int j0 = (tile - cached) * CAM_NEW;
+          constexpr int CH = D / 8;
+          for (int i = tid; i < 2 * CAM_NEW * CH; i += CAM_THREADS) {
+            const int which = i / (CAM_NEW * CH), r = i / CH % CAM_NEW, ch = i % CH;
+            const int x = ((r & 3) << 1) | ((r >> 2) & 1);
+            const bool in = j0 + r < R;
+            const T* src = which ? static_cast<const T*>(a.v) + (long long)(r0 + (in ? j0 + r : 0)) * a.v_row + kvh * a.v_head
+                                 : static_cast<const T*>(a.k) + (long long)(r0 + (in ? j0 + r : 0)) * a.k_row + kvh * a.k_head;
+            cp_async16(smem_u32(st) + (which * CAM_NEW + r) * D * 2 + ((ch ^ x) << 4), src + ch * 8, in ? 16 : 0);
+          }
+        }
+      }
+      cp_async_commit();
+    };
+    __syncthreads();                             // (the last unit's merge has read the stages)
+#pragma unroll
+    for (int i = 0; i < ST - 1; ++i) {
+      if (ALONE && tile0 + i >= cached) __syncthreads();
+      issue(tile0 + i);
+    }
+
+    // ---- the warp's 16 rows of q: lane (g, t) holds dims 16 i + 4 t .. + 3 of rows g and g + 8
+    int qi[2], qh[2];
+    bool live[2];
+    uint32_t qf[DC][4];
+    float rs[2];
+    auto load_q = [&](uint32_t (&f)[DC][4]) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const T* qp = static_cast<const T*>(a.q) + (long long)(r0 + qi[e]) * a.q_row + (long long)qh[e] * a.q_head + 4 * t4;
+#pragma unroll
+        for (int i = 0; i < DC; ++i) {
+          const uint2 w = live[e] ? *reinterpret_cast<const uint2*>(qp + 16 * i) : make_uint2(0, 0);
+          f[i][e] = w.x;
+          f[i][2 + e] = w.y;
+        }
+      }
+    };
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int m = rtile * MT + rg * 16 + g + 8 * e;
+      qi[e] = m / G;
+      qh[e] = kvh * G + m % G;
+      live[e] = qi[e] < R;
+    }
+    load_q(qf);
+    const float scale2 = a.scale * 1.44269504088896f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      float back = 1.f;
+      if constexpr (std::is_same<T, bf16>::value) {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < DC; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float2 v = unpack2<T>(qf[i][2 * h + e]);
+            top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+          }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int ex = (int)(__float_as_uint(top) >> 23);                 // largest value into [2^8, 2^9)
+        const int up = ex == 0 || ex == 255 ? 0 : max(-120, min(120, 135 - ex));
+        const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+        back = __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+        for (int i = 0; i < DC; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float2 v = unpack2<T>(qf[i][2 * h + e]);
+            qf[i][2 * h + e] = pack2<f16>(v.x * f, v.y * f);
+          }
+      }
+      rs[e] = back * scale2 * code_unit<FMT>();
+    }
+
+    float o[DT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    // new maxima of the two rows: the sums so far move to the new reference
+    auto raise = [&](float (&top)[2], float (&ref)[2]) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 1));
+        top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], 2));
+        top[e] = fmaxf(top[e], m[e]);
+        ref[e] = top[e] == -INFINITY ? 0.f : top[e];
+      }
+      if (__any_sync(0xffffffffu, top[0] > m[0] || top[1] > m[1])) {
+        const float f0 = ex2(m[0] - ref[0]), f1 = ex2(m[1] - ref[1]);
+        l[0] *= f0;
+        l[1] *= f1;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          o[i][0] *= f0;
+          o[i][1] *= f0;
+          o[i][2] *= f1;
+          o[i][3] *= f1;
+        }
+        m[0] = top[0];
+        m[1] = top[1];
+      }
+    };
+
+    // ---- cached tiles
+    int tile = tile0;
+    for (; tile < min(tile1, cached); ++tile) {
+      if (ALONE) {
+        if (tile + ST - 1 >= cached && tile + ST - 1 < tile1) __syncthreads();
+        cp_async_wait<ST - 2>();
+        __syncwarp();
+      } else {
+        cp_async_wait<ST - 2>();
+        __syncthreads();
+      }
+      issue(tile + ST - 1);
+      const uint8_t* st = smem + (tile % ST) * STAGE;
+      const float2* sc = reinterpret_cast<const float2*>(st + 256 * D) + kg * NP;
+      const uint32_t base = smem_u32(st) + kg * NP * 2 * BLOCK + lane * 16;
+      const int key0 = tile * CAM_TILE + kg * NP * CACHE_PAGE;
+      constexpr int STEP = NP > 2 ? 2 : NP;      // pages a softmax step
+#pragma unroll 1
+      for (int pg = 0; pg < NP; pg += STEP) {
+        if (key0 + pg * CACHE_PAGE >= n) break;
+        float sv[2 * STEP][4], inv[STEP], lg[STEP];
+        float top[2] = {-INFINITY, -INFINITY}, ref[2];
+#pragma unroll
+        for (int u = 0; u < STEP; ++u) {
+          const float2 f = sc[pg + u];
+          const float v = f.y > 0.f ? f.y * code_unit<FMT>() : 9.094947017729282e-13f;   // (a block of zeros: any factor would do; 2^-40 does not raise the reference)
+          lg[u] = __log2f(v);
+          inv[u] = __fdividef(1.f, v);
+          const float f0 = rs[0] * f.x, f1 = rs[1] * f.x;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float (&x)[4] = sv[2 * u + h];
+            x[0] = x[1] = x[2] = x[3] = 0.f;
+#pragma unroll
+            for (int i = 0; i < DC; i += 4) {
+              uint32_t w[4];
+              cam_ldsm4(base + (pg + u) * 2 * BLOCK + h * 8 * D + i * 128, w);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                uint32_t b0, b1;
+                codes_to_f16<FMT>(w[j], b0, b1);
+                cam_mma<f16>(x, qf[i + j], b0, b1);
+              }
+            }
+            x[0] = x[0] * f0 + lg[u];
+            x[1] = x[1] * f0 + lg[u];
+            x[2] = x[2] * f1 + lg[u];
+            x[3] = x[3] * f1 + lg[u];
+            const int key = key0 + (pg + u) * CACHE_PAGE + 8 * h + 2 * t4;
+            if (key >= n) x[0] = x[2] = -INFINITY;
+            if (key + 1 >= n) x[1] = x[3] = -INFINITY;
+            top[0] = fmaxf(top[0], fmaxf(x[0], x[1]));
+            top[1] = fmaxf(top[1], fmaxf(x[2], x[3]));
+          }
+        }
+        raise(top, ref);
+#pragma unroll
+        for (int u = 0; u < STEP; ++u) {
+          float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float (&x)[4] = sv[2 * u + h];
+            x[0] = ex2(x[0] - ref[0]);
+            x[1] = ex2(x[1] - ref[0]);
+            x[2] = ex2(x[2] - ref[1]);
+            x[3] = ex2(x[3] - ref[1]);
+            s0 += x[0] + x[1];
+            s1 += x[2] + x[3];
+          }
+          l[0] += s0 * inv[u];
+          l[1] += s1 * inv[u];
+          const uint32_t p[4] = {pack2<T>(sv[2 * u][0], sv[2 * u][1]), pack2<T>(sv[2 * u][2], sv[2 * u][3]), pack2<T>(sv[2 * u + 1][0], sv[2 * u + 1][1]),
+                                 pack2<T>(sv[2 * u + 1][2], sv[2 * u + 1][3])};
+#pragma unroll
+          for (int i = 0; i < DT; i += 4) {
+            uint32_t w[4];
+            cam_ldsm4(base + (pg + u) * 2 * BLOCK + BLOCK + i * 128, w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t b0, b1;
+              codes_to<FMT, T>(w[j], b0, b1);
+              cam_mma<T>(o[i + j], p, b0, b1);
+            }
+          }
+        }
+      }
+    }
+
+    // ---- rows of the pass
+    if (tile < tile1) {
+      load_q(qf);
+      float cv = 1.f;
+      if (n > 0) {
+        const int page = c.page(s, 0);
+        const float f = page >= 0 ? c.scales[(head_block + page) * 2 + 1] * code_unit<FMT>() : 0.f;
+        if (f > 0.f) cv = std::is_same<T, bf16>::value ? f : fmaxf(f, 3.0517578125e-5f);   // (float16 weights w' / c stay below 2^15)
+      }
+      const float lgc = __log2f(cv), invc = __fdividef(1.f, cv);
+      for (; tile < tile1; ++tile) {
+        cp_async_wait<ST - 2>();
+        __syncthreads();
+        issue(tile + ST - 1);
+        const uint8_t* st = smem + (tile % ST) * STAGE;
+        const int nt = tile - cached;
+        unsigned long long vis[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) vis[e] = live[e] ? sees64(a.mask, a.mask_words, (size_t)(r0 + qi[e]), qi[e], nt, R) : 0ull;
+#pragma unroll 1
+        for (int ch = kg; ch < CAM_NEW / 16; ch += KG) {
+          if (__all_sync(0xffffffffu, (((vis[0] | vis[1]) >> (16 * ch)) & 0xffff) == 0)) continue;
+          float x[2][4];
+          float top[2] = {-INFINITY, -INFINITY}, ref[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            x[h][0] = x[h][1] = x[h][2] = x[h][3] = 0.f;
+            const int r = 16 * ch + 8 * h + g, sw = ((r & 3) << 1) | ((r >> 2) & 1);
+#pragma unroll
+            for (int i = 0; i < DC; ++i) {
+              const uint2 w = *reinterpret_cast<const uint2*>(st + r * D * 2 + (((2 * i + (t4 >> 1)) ^ sw) << 4) + (t4 & 1) * 8);
+              cam_mma<T>(x[h], qf[i], w.x, w.y);
+            }
+            const int k = 16 * ch + 8 * h + 2 * t4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[h][e] = (vis[e >> 1] >> (k + (e & 1))) & 1 ? x[h][e] * scale2 + lgc : -INFINITY;
+            top[0] = fmaxf(top[0], fmaxf(x[h][0], x[h][1]));
+            top[1] = fmaxf(top[1], fmaxf(x[h][2], x[h][3]));
+          }
+          raise(top, ref);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[h][e] = ex2(x[h][e] - ref[e >> 1]) * invc;
+              l[e >> 1] += x[h][e];
+            }
+          const uint32_t p[4] = {pack2<T>(x[0][0], x[0][1]), pack2<T>(x[0][2], x[0][3]), pack2<T>(x[1][0], x[1][1]), pack2<T>(x[1][2], x[1][3])};
+          bool odd = false;
+#pragma unroll
+          for (int i = 0; i < DT; i += 2) {
+            uint32_t w[4];
+            const int r = 16 * ch + (lane & 15), sw = ((r & 3) << 1) | ((r >> 2) & 1);
+            cam_ldsm4_trans(smem_u32(st) + (CAM_NEW + r) * D * 2 + (((i + (lane >> 4)) ^ sw) << 4), w);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (odd2<T>(w[j])) {
+                odd = true;
+                w[j] = tame2<T>(w[j]);
+              }
+            cam_mma<T>(o[i], p, w[0], w[1]);
+            cam_mma<T>(o[i + 1], p, w[2], w[3]);
+          }
+          if (__any_sync(0xffffffffu, odd)) {
+            // infinities and NaN among these rows of v: they reach the rows that see them, and only those
+#pragma unroll 1
+            for (int k = 0; k < 16; ++k) {
+              const int r = 16 * ch + k, sw = ((r & 3) << 1) | ((r >> 2) & 1), from = (lane & ~3) | ((k & 7) >> 1);
+              float pk[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float y0 = __shfl_sync(0xffffffffu, x[0][2 * e], from), y1 = __shfl_sync(0xffffffffu, x[0][2 * e + 1], from);
+                const float y2 = __shfl_sync(0xffffffffu, x[1][2 * e], from), y3 = __shfl_sync(0xffffffffu, x[1][2 * e + 1], from);
+                pk[e] = k < 8 ? (k & 1 ? y1 : y0) : (k & 1 ? y3 : y2);
+              }
+#pragma unroll
+              for (int i = 0; i < DT; ++i) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(st + (CAM_NEW + r) * D * 2 + ((i ^ sw) << 4) + t4 * 4);
+                if (!odd2<T>(w)) continue;
+                const float2 all = unpack2<T>(w);
+                const bool ox = !(fabsf(all.x) < INFINITY), oy = !(fabsf(all.y) < INFINITY);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  if ((vis[e] >> r) & 1) {
+                    if (ox) o[i][2 * e] += pk[e] * all.x;
+                    if (oy) o[i][2 * e + 1] += pk[e] * all.y;
+                  }
+              }
+            }
+          }
+        }
+      }
+    }
+    cp_async_wait<0>();
+    __syncthreads();
+
+    // ---- the key groups' sums through shared memory: [kg][row][D] and (max, sum)
+    float* so = reinterpret_cast<float*>(smem);
+    float* sm = so + KG * MT * D;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
+      l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
+      const int r = rg * 16 + g + 8 * e;
+      if (t4 == 0) {
+        sm[(kg * MT + r) * 2] = m[e];
+        sm[(kg * MT + r) * 2 + 1] = l[e];
+      }
+#pragma unroll
+      for (int i = 0; i < DT; ++i) *reinterpret_cast<float2*>(so + (kg * MT + r) * D + 8 * i + 2 * t4) = make_float2(o[i][2 * e], o[i][2 * e + 1]);
+    }
+    __syncthreads();
+    const bool whole = tile0 == 0 && tile1 == tiles;
+    const int unit = (b * pl.nrt + rt) * c.kv + kvh;
+    // a row's D values by D / 4 threads; `parts` sums behind one another, weighed by their maxima
+    auto finish = [&](int r, int d, float top, float sum, float4 v) {
+      const int mm = rtile * MT + r, i = mm / G, h = kvh * G + mm % G;
+      if (i >= R) return;
+      const float f = sum > 0.f || sum != sum ? 1.f / sum : 0.f;      // (a sum that is NaN makes the row NaN)
+      uint2 w = make_uint2(pack2<T>(v.x * f, v.y * f), pack2<T>(v.z * f, v.w * f));
+      const size_t row = (size_t)(r0 + i) * a.H + h;
+      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + row * D + d) = w;
+      if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.693147180559945f;
+    };
+    for (int x = tid; x < MT * D / 4; x += CAM_THREADS) {
+      const int r = x / (D / 4), d = x % (D / 4) * 4;
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < KG; ++k) top = fmaxf(top, sm[(k * MT + r) * 2]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float sum = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < KG; ++k) {
+        const float f = ex2(sm[(k * MT + r) * 2] - ref);
+        const float4 y = *reinterpret_cast<const float4*>(so + (k * MT + r) * D + d);
+        sum += f * sm[(k * MT + r) * 2 + 1];
+        v.x += f * y.x;
+        v.y += f * y.y;
+        v.z += f * y.z;
+        v.w += f * y.w;
+      }
+      if (whole) {
+        finish(r, d, top, sum, v);
+      } else {
+        float* out = pl.part + ((size_t)blockIdx.x * 2 + (at == run0 ? 0 : 1)) * (MT * (D + 2));
+        *reinterpret_cast<float4*>(out + r * D + d) = v;
+        if (d == 0) {
+          out[MT * D + 2 * r] = top;
+          out[MT * D + 2 * r + 1] = sum;
+        }
+      }
+    }
+    if (!whole) {
+      const long long c0 = owner(unit0), c1 = owner(unit0 + tiles - 1);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const int before = atomicAdd(pl.arrive + unit, 1);
+        last = before == (int)(c1 - c0);
+        if (last) pl.arrive[unit] = 0;
+      }
+      __syncthreads();
+      if (last) {
+        __threadfence();
+        for (int x = tid; x < MT * D / 4; x += CAM_THREADS) {
+          const int r = x / (D / 4), d = x % (D / 4) * 4;
+          float top = -INFINITY, sum = 0.f;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (long long k = c0; k <= c1; ++k) {
+            const float* in = pl.part + ((size_t)k * 2 + (run_begin(k) < unit0 ? 1 : 0)) * (MT * (D + 2));
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(in + MT * D + 2 * r));
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(in + r * D + d));
+            const float now = fmaxf(top, ml.x), ref = now == -INFINITY ? 0.f : now;
+            const float f = ex2(top - ref), h = ex2(ml.x - ref);
+            sum = f * sum + h * ml.y;
+            v.x = f * v.x + h * y.x;
+            v.y = f * v.y + h * y.y;
+            v.z = f * v.z + h * y.z;
+            v.w = f * v.w + h * y.w;
+            top = now;
+          }
+          finish(r, d, top, sum, v);
+        }
+      }
+    }
+    at += tile1 - tile0;
+  }
 }
 
 }  // namespace spec
