@@ -78,14 +78,14 @@ AttnShape attn_shape(const spec_cache* c, int n_heads, int batch, int max_rows) 
   s.tiles = (rows + s.mt - 1) / s.mt;
   s.pairs = s.tiles * batch < CAM_PAIRS ? s.tiles * batch : CAM_PAIRS;
   s.arrive_bytes = ((size_t)s.pairs * c->n_kv_heads * 4 + 255) / 256 * 256;
-  s.bytes = s.arrive_bytes + (size_t)2 * CAM_SMS * 2 * s.mt * (c->head_dim + 2) * 4;
+  s.bytes = s.arrive_bytes + (size_t)CAM_SMS * 2 * s.mt * (c->head_dim + 2) * 4;
   return s;
 }
 template <typename T, int D, int FMT, int RG> int launch_mma(const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
   auto kernel = cache_attention_mma<T, D, FMT, RG>;
-  const size_t smem = cam_smem(D, RG);
+  const size_t smem = cam_smem(D);
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return launched("spec_cache_attention: shared memory");
-  kernel<<<CAM_SMS * (RG == 4 ? 1 : 2), CAM_THREADS, smem, st>>>(a, pl);
+  kernel<<<CAM_SMS, CAM_THREADS, smem, st>>>(a, pl);
   return launched("spec_cache_attention");
 }
 unsigned copy_blocks(size_t units) {

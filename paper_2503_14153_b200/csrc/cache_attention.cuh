@@ -134,10 +134,13 @@ __global__ void __launch_bounds__(CAS_THREADS) cache_attention_simple(CacheAttnA
 // of V as they are, w' is at most 1, and the sum of the weights adds w' / sv. So pages of any scale share one accumulator. Rows of the pass count as a page of scale c, the sequence's first
 // page's, and their weights are w' / c in the operand type.
 //
-// Work: every CTA gets an equal run of consecutive tiles of the list of all units (sequence, head, row tile), which it works out from the lengths in device memory; a unit cut by the
+// Work: one CTA an SM; every CTA gets an equal run of consecutive slots of the list of all units (sequence, head, row tile), which it works out from the lengths in device memory. A unit
+// is CAM_UNIT slots that stand for its fixed cost (q, the merge, the output), then its tiles. The fetches run ahead of the sums across the ends of units. A unit cut by the
 // end of a run leaves (max, sum, values) in scratch and the last of its CTAs to arrive adds the parts in the order of the CTAs.
 constexpr int CAM_WARPS = 8, CAM_THREADS = 32 * CAM_WARPS;
 constexpr int CAM_TILE = 128, CAM_PAGES = CAM_TILE / CACHE_PAGE, CAM_NEW = 64;   // cached tokens and rows of the pass a tile
+constexpr int CAM_STAGES = 4;
+constexpr int CAM_UNIT = 2;
 constexpr int CAM_PAIRS = 4096;          // (sequence, row tile) pairs a launch can deal
 constexpr int CAM_SMS = 148;
 
@@ -148,8 +151,8 @@ struct CamPlan {
 };
 
 __host__ __device__ constexpr int cam_stage_bytes(int D) { return 256 * D + 128; }
-__host__ __device__ constexpr int cam_stages(int RG) { return 3; }
-__host__ __device__ constexpr size_t cam_smem(int D, int RG) { return (size_t)cam_stages(RG) * cam_stage_bytes(D); }
+// ring, then the key groups' sums: [KG][MT][D] values and (max, sum) pairs
+__host__ __device__ constexpr size_t cam_smem(int D) { return (size_t)CAM_STAGES * cam_stage_bytes(D) + (size_t)CAM_WARPS * 16 * (D + 2) * 4; }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -250,9 +253,26 @@ __device__ __forceinline__ unsigned long long sees64(const uint32_t* mask, int w
   return left >= 64 ? v : left <= 0 ? 0ull : v & ((1ull << left) - 1);
 }
 
+// The dealing of slots to CTAs: an even split, 32-bit arithmetic where it suffices.
+struct CamDeal {
+  long long total;
+  int ctas;
+  bool small;
+  __device__ __forceinline__ long long begin(int cta) const { return small ? (long long)((uint32_t)cta * (uint32_t)total / (uint32_t)ctas) : (long long)cta * total / ctas; }
+  __device__ __forceinline__ int owner(long long slot) const {
+    return small ? (int)(((uint32_t)(slot + 1) * (uint32_t)ctas - 1) / (uint32_t)total) : (int)(((slot + 1) * ctas - 1) / total);
+  }
+};
+
+// A place in the list of units: the unit and the tiles of it that this CTA has left.
+struct CamCursor {
+  int b, kvh, rt, tile, tile1, tiles, cached, n, s, r0, R;
+  long long unit0;                       // first slot of the unit
+};
+
 template <typename T, int D, int FMT, int RG>
-__global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_mma(CacheAttnArgs a, CamPlan pl) {
-  constexpr int KG = CAM_WARPS / RG, MT = 16 * RG, ST = cam_stages(RG), NP = CAM_PAGES / KG;
+__global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnArgs a, CamPlan pl) {
+  constexpr int KG = CAM_WARPS / RG, MT = 16 * RG, ST = CAM_STAGES, NP = CAM_PAGES / KG;
   constexpr int DC = D / 16, DT = D / 8, STAGE = cam_stage_bytes(D), BLOCK = CACHE_PAGE * D;
   constexpr bool ALONE = RG == 1;                // a warp uses only the pages it fetched itself
   extern __shared__ __align__(128) uint8_t smem[];
@@ -264,28 +284,34 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
   const int rg = warp % RG, kg = warp / RG;
   const int G = a.H / c.kv, pairs = pl.nb * pl.nrt;
 
-  // ---- the list of units: tiles of every (sequence, row tile), one kv head; prefix sums
-  auto rows_of = [&](int b, int& r0) {
-    r0 = rows_begin(a.row_offsets, b, a.rows, a.batch);
-    return max(0, rows_begin(a.row_offsets, b + 1, a.rows, a.batch) - r0);
-  };
-  auto tiles_of = [&](int pair, int& cached) {
-    const int b = pl.b0 + pair / pl.nrt, rt = pl.rt0 + pair % pl.nrt;
-    int r0;
-    const int R = rows_of(b, r0), left = R * G - rt * MT;
-    cached = 0;
-    if (left <= 0) return 0;
-    const int s = c.sequence(a.seqs, b);
-    cached = s < 0 ? 0 : (c.len(s) + CAM_TILE - 1) / CAM_TILE;
-    const int seen = a.mask ? R : min(R, (rt * MT + min(left, MT) - 1) / G + 1);
-    return cached + (seen + CAM_NEW - 1) / CAM_NEW;
+  // ---- the list of units: slots of every (sequence, row tile), one kv head; prefix sums
+  auto fill = [&](CamCursor& u) {                // the numbers of unit (b, rt)
+    const int b = pl.b0 + u.b, m0 = (pl.rt0 + u.rt) * MT;
+    u.r0 = rows_begin(a.row_offsets, b, a.rows, a.batch);
+    u.R = max(0, rows_begin(a.row_offsets, b + 1, a.rows, a.batch) - u.r0);
+    const int left = u.R * G - m0;
+    u.cached = u.tiles = u.n = 0;
+    u.s = -1;
+    if (left <= 0) return;
+    u.s = c.sequence(a.seqs, b);
+    u.n = u.s < 0 ? 0 : c.len(u.s);
+    u.cached = (u.n + CAM_TILE - 1) / CAM_TILE;
+    const int seen = a.mask ? u.R : min(u.R, (m0 + min(left, MT) - 1) / G + 1);
+    u.tiles = u.cached + (seen + CAM_NEW - 1) / CAM_NEW;
   };
   {
     const int each = (pairs + CAM_THREADS - 1) / CAM_THREADS;
-    int mine = 0, dummy;
+    int mine = 0;
     for (int i = 0; i < each; ++i) {
       const int p = tid * each + i;
-      if (p < pairs) mine += tiles_of(p, dummy);
+      if (p < pairs) {
+        CamCursor u;
+        u.b = p / pl.nrt;
+        u.rt = p - u.b * pl.nrt;
+        fill(u);
+        pre[p] = u.tiles ? u.tiles + CAM_UNIT : 0;
+        mine += pre[p];
+      }
     }
     int x = mine;
 #pragma unroll
@@ -300,94 +326,133 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
     for (int i = 0; i < each; ++i) {
       const int p = tid * each + i;
       if (p < pairs) {
+        const int w = pre[p];
         pre[p] = at;
-        at += tiles_of(p, dummy);
+        at += w;
         if (p == pairs - 1) pre[pairs] = at;
       }
     }
     __syncthreads();
   }
-  const long long total = (long long)pre[pairs] * c.kv;
-  const long long ctas = min((long long)gridDim.x, total);
-  if (blockIdx.x >= ctas) return;
-  auto run_begin = [&](long long cta) { return cta * total / ctas; };
-  auto owner = [&](long long tile) { return ((tile + 1) * ctas - 1) / total; };
-  const long long run0 = run_begin(blockIdx.x), run1 = run_begin(blockIdx.x + 1ll);
+  CamDeal deal;
+  deal.total = (long long)pre[pairs] * c.kv;
+  deal.ctas = (int)min((long long)gridDim.x, deal.total);
+  deal.small = deal.total < (1 << 23);
+  if ((int)blockIdx.x >= deal.ctas) return;
+  const long long run0 = deal.begin(blockIdx.x), run1 = deal.begin(blockIdx.x + 1);
 
-  for (long long at = run0; at < run1;) {
-    // ---- which unit
-    int b, kvh, rt, tile0, tiles;
-    long long unit0;
-    {
-      int lo = 0, hi = pl.nb;                    // sequence: the last one whose units begin at or before `at` and that has any
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((long long)pre[mid * pl.nrt] * c.kv <= at) lo = mid; else hi = mid;
-      }
-      b = lo;
-      const int p0 = b * pl.nrt, w = pre[p0 + pl.nrt] - pre[p0];
-      const long long in = at - (long long)pre[p0] * c.kv;
-      kvh = (int)(in / w);
-      const int r = (int)(in % w) + pre[p0];
-      lo = p0, hi = p0 + pl.nrt;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (pre[mid] <= r) lo = mid; else hi = mid;
-      }
-      rt = lo - p0;
-      tiles = pre[lo + 1] - pre[lo];
-      tile0 = r - pre[lo];
-      unit0 = at - tile0;
-    }
-    const int tile1 = (int)min((long long)tiles, tile0 + (run1 - at));
-    const int seq_b = pl.b0 + b, rtile = pl.rt0 + rt;
-    int r0, cached;
-    const int R = rows_of(seq_b, r0);
-    tiles_of(b * pl.nrt + rt, cached);
-    const int s = c.sequence(a.seqs, seq_b);
-    const int n = s < 0 ? 0 : c.len(s);
-    const size_t head_block = ((size_t)a.layer * c.kv + kvh) * c.n_pages;
-
-    // ---- fetches: one group of copies a tile
-    auto issue = [&](int tile) {
-      if (tile < tile1) {
-        uint8_t* st = smem + (tile % ST) * STAGE;
-        if (tile < cached) {
-          // a warp a page
-          const int p = tile * CAM_PAGES + warp;
-          const uint32_t dst = smem_u32(st + warp * 2 * BLOCK) + lane * 16;
-          float2* sc = reinterpret_cast<float2*>(st + 256 * D) + warp;
-          const int page = p * CACHE_PAGE < n ? c.page(s, p) : -1;
-          if (page >= 0) {
-            const uint8_t* src = c.codes + (head_block + page) * (2 * BLOCK) + lane * 16;
-#pragma unroll
-            for (int i = 0; i < 2 * BLOCK / 512; ++i) cp_async16(dst + i * 512, src + i * 512, 16);
-            if (lane == 0) cp_async8(smem_u32(sc), c.scales + (head_block + page) * 2);
-          } else if (lane == 0) {
-            *sc = make_float2(0.f, 0.f);
-          }
-        } else {
-          // 64 rows of k, then of v; 16-byte chunk ch of row r at chunk ch ^ x(r)
-          const int j0 = (tile - cached) * CAM_NEW;
-          constexpr int CH = D / 8;
-          for (int i = tid; i < 2 * CAM_NEW * CH; i += CAM_THREADS) {
-            const int which = i / (CAM_NEW * CH), r = i / CH % CAM_NEW, ch = i % CH;
-            const int x = ((r & 3) << 1) | ((r >> 2) & 1);
-            const bool in = j0 + r < R;
-            const T* src = which ? static_cast<const T*>(a.v) + (long long)(r0 + (in ? j0 + r : 0)) * a.v_row + kvh * a.v_head
-                                 : static_cast<const T*>(a.k) + (long long)(r0 + (in ? j0 + r : 0)) * a.k_row + kvh * a.k_head;
-            cp_async16(smem_u32(st) + (which * CAM_NEW + r) * D * 2 + ((ch ^ x) << 4), src + ch * 8, in ? 16 : 0);
+  // the first tile of the run, or the next one; false when the run is over
+  auto enter = [&](CamCursor& u, long long at) {   // at: a slot of the unit, u.unit0 its first
+    fill(u);
+    u.tile = max(0, (int)(at - u.unit0) - CAM_UNIT);
+    u.tile1 = (int)min((long long)u.tiles, run1 - u.unit0 - CAM_UNIT);
+  };
+  auto next_unit = [&](CamCursor& u) {
+    long long at = u.unit0 + u.tiles + CAM_UNIT;
+    do {
+      if (at >= run1) return false;
+      do {
+        if (++u.rt == pl.nrt) {
+          u.rt = 0;
+          if (++u.kvh == c.kv) {
+            u.kvh = 0;
+            ++u.b;
           }
         }
-      }
-      cp_async_commit();
-    };
-    __syncthreads();                             // (the last unit's merge has read the stages)
-#pragma unroll
-    for (int i = 0; i < ST - 1; ++i) {
-      if (ALONE && tile0 + i >= cached) __syncthreads();
-      issue(tile0 + i);
+      } while (pre[u.b * pl.nrt + u.rt + 1] == pre[u.b * pl.nrt + u.rt]);
+      u.unit0 = at;
+      enter(u, at);
+      at += u.tiles + CAM_UNIT;
+    } while (u.tile >= u.tile1);
+    return true;
+  };
+  CamCursor use;
+  {
+    int lo = 0, hi = pl.nb;                      // the last sequence whose units begin at or before the run (one without units begins where the next one does)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((long long)pre[mid * pl.nrt] * c.kv <= run0) lo = mid; else hi = mid;
     }
+    use.b = lo;
+    const int p0 = lo * pl.nrt, w = pre[p0 + pl.nrt] - pre[p0];
+    const long long in = run0 - (long long)pre[p0] * c.kv;
+    use.kvh = deal.small ? (int)((uint32_t)in / (uint32_t)w) : (int)(in / w);
+    const int r = (int)(in - (long long)use.kvh * w) + pre[p0];
+    lo = p0, hi = p0 + pl.nrt;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pre[mid] <= r) lo = mid; else hi = mid;
+    }
+    use.rt = lo - p0;
+    use.unit0 = run0 - (r - pre[lo]);
+    enter(use, run0);
+    if (use.tile >= use.tile1 && !next_unit(use)) return;
+  }
+  CamCursor get = use;
+  bool more = true;                              // `get` stands at a tile
+
+  // ---- fetches: one group of copies a tile. The page number of the tile after is asked for a step ahead.
+  auto page_of = [&](const CamCursor& u) {
+    const int p = u.tile * CAM_PAGES + warp;
+    return u.tile < u.cached && p * CACHE_PAGE < u.n ? c.page(u.s, p) : -1;
+  };
+  int page = page_of(get), slot = 0;
+  auto issue = [&]() {
+    if (more) {
+      uint8_t* st = smem + slot * STAGE;
+      if (get.tile < get.cached) {
+        // a warp a page
+        const uint32_t dst = smem_u32(st + warp * 2 * BLOCK) + lane * 16;
+        float2* sc = reinterpret_cast<float2*>(st + 256 * D) + warp;
+        if (page >= 0) {
+          const size_t blk = ((size_t)a.layer * c.kv + get.kvh) * c.n_pages + page;
+          const uint8_t* src = c.codes + blk * (2 * BLOCK) + lane * 16;
+#pragma unroll
+          for (int i = 0; i < 2 * BLOCK / 512; ++i) cp_async16(dst + i * 512, src + i * 512, 16);
+          if (lane == 0) cp_async8(smem_u32(sc), c.scales + blk * 2);
+        } else if (lane == 0) {
+          *sc = make_float2(0.f, 0.f);
+        }
+      } else {
+        // up to 64 rows of k, then of v; 16-byte chunk ch of row r at chunk ch ^ x(r). Rows up to the next multiple of 16 are filled up with zeros
+        const int j0 = (get.tile - get.cached) * CAM_NEW, rows = min(CAM_NEW, (get.R - j0 + 15) & ~15);
+        constexpr int CH = D / 8;
+        for (int i = tid; i < 2 * rows * CH; i += CAM_THREADS) {
+          const int which = i >= rows * CH, r = i / CH - which * rows, ch = i % CH;
+          const int x = ((r & 3) << 1) | ((r >> 2) & 1);
+          const bool in = j0 + r < get.R;
+          const long long row = get.r0 + (in ? j0 + r : 0);
+          const T* src = which ? static_cast<const T*>(a.v) + row * a.v_row + get.kvh * a.v_head : static_cast<const T*>(a.k) + row * a.k_row + get.kvh * a.k_head;
+          cp_async16(smem_u32(st) + (which * CAM_NEW + r) * D * 2 + ((ch ^ x) << 4), src + ch * 8, in ? 16 : 0);
+        }
+      }
+      if (++slot == ST) slot = 0;
+      if (++get.tile == get.tile1) more = next_unit(get);
+      if (more) page = page_of(get);
+    }
+    cp_async_commit();
+  };
+#pragma unroll 1
+  for (int i = 0; i < ST - 1; ++i) issue();      // (into an empty ring)
+
+  const float scale2 = a.scale * 1.44269504088896f;
+  int at_slot = 0;
+  bool was_new = false;
+  // The next tile's data is there, and the stage that the next fetch goes to is free. A warp that uses only pages of its own fetching need not meet the others, unless rows of the pass, which all
+  // warps fetch, are used, were used a step ago or are fetched next.
+  auto step = [&](bool is_new) {
+    cp_async_wait<ST - 2>();
+    if (!ALONE || is_new || was_new || (more && get.tile >= get.cached)) __syncthreads();
+    else __syncwarp();
+    was_new = is_new;
+    issue();
+    const uint8_t* st = smem + at_slot * STAGE;
+    if (++at_slot == ST) at_slot = 0;
+    return st;
+  };
+
+  for (bool go = true; go; go = next_unit(use)) {
+    const int R = use.R, n = use.n, kvh = use.kvh, r0 = use.r0, cached = use.cached, tile1 = use.tile1, tile0 = use.tile, rtile = pl.rt0 + use.rt;
 
     // ---- the warp's 16 rows of q: lane (g, t) holds dims 16 i + 4 t .. + 3 of rows g and g + 8
     int qi[2], qh[2];
@@ -413,37 +478,6 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
       qh[e] = kvh * G + m % G;
       live[e] = qi[e] < R;
     }
-    load_q(qf);
-    const float scale2 = a.scale * 1.44269504088896f;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float back = 1.f;
-      if constexpr (std::is_same<T, bf16>::value) {
-        float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < DC; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float2 v = unpack2<T>(qf[i][2 * h + e]);
-            top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
-          }
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int ex = (int)(__float_as_uint(top) >> 23);                 // largest value into [2^8, 2^9)
-        const int up = ex == 0 || ex == 255 ? 0 : max(-120, min(120, 135 - ex));
-        const float f = __uint_as_float((uint32_t)(127 + up) << 23);
-        back = __uint_as_float((uint32_t)(127 - up) << 23);
-#pragma unroll
-        for (int i = 0; i < DC; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float2 v = unpack2<T>(qf[i][2 * h + e]);
-            qf[i][2 * h + e] = pack2<f16>(v.x * f, v.y * f);
-          }
-      }
-      rs[e] = back * scale2 * code_unit<FMT>();
-    }
-
     float o[DT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -474,17 +508,40 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
 
     // ---- cached tiles
     int tile = tile0;
-    for (; tile < min(tile1, cached); ++tile) {
-      if (ALONE) {
-        if (tile + ST - 1 >= cached && tile + ST - 1 < tile1) __syncthreads();
-        cp_async_wait<ST - 2>();
-        __syncwarp();
-      } else {
-        cp_async_wait<ST - 2>();
-        __syncthreads();
+    if (tile < cached) {
+      load_q(qf);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float back = 1.f;
+        if constexpr (std::is_same<T, bf16>::value) {
+          float top = 0.f;
+#pragma unroll
+          for (int i = 0; i < DC; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float2 v = unpack2<T>(qf[i][2 * h + e]);
+              top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+            }
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const int ex = (int)(__float_as_uint(top) >> 23);                 // largest value into [2^8, 2^9)
+          const int up = ex == 0 || ex == 255 ? 0 : max(-120, min(120, 135 - ex));
+          const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+          back = __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+          for (int i = 0; i < DC; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float2 v = unpack2<T>(qf[i][2 * h + e]);
+              qf[i][2 * h + e] = pack2<f16>(v.x * f, v.y * f);
+            }
+        }
+        rs[e] = back * scale2 * code_unit<FMT>();
       }
-      issue(tile + ST - 1);
-      const uint8_t* st = smem + (tile % ST) * STAGE;
+    }
+#pragma unroll 1
+    for (; tile < min(tile1, cached); ++tile) {
+      const uint8_t* st = step(false);
       const float2* sc = reinterpret_cast<const float2*>(st + 256 * D) + kg * NP;
       const uint32_t base = smem_u32(st) + kg * NP * 2 * BLOCK + lane * 16;
       const int key0 = tile * CAM_TILE + kg * NP * CACHE_PAGE;
@@ -494,6 +551,7 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
         if (key0 + pg * CACHE_PAGE >= n) break;
         float sv[2 * STEP][4], inv[STEP], lg[STEP];
         float top[2] = {-INFINITY, -INFINITY}, ref[2];
+        const bool cut = key0 + (pg + STEP) * CACHE_PAGE > n;
 #pragma unroll
         for (int u = 0; u < STEP; ++u) {
           const float2 f = sc[pg + u];
@@ -504,6 +562,7 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float (&x)[4] = sv[2 * u + h];
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
             x[0] = x[1] = x[2] = x[3] = 0.f;
 #pragma unroll
             for (int i = 0; i < DC; i += 4) {
@@ -513,16 +572,18 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
               for (int j = 0; j < 4; ++j) {
                 uint32_t b0, b1;
                 codes_to_f16<FMT>(w[j], b0, b1);
-                cam_mma<f16>(x, qf[i + j], b0, b1);
+                cam_mma<f16>(j & 1 ? y : x, qf[i + j], b0, b1);         // (two chains)
               }
             }
-            x[0] = x[0] * f0 + lg[u];
-            x[1] = x[1] * f0 + lg[u];
-            x[2] = x[2] * f1 + lg[u];
-            x[3] = x[3] * f1 + lg[u];
-            const int key = key0 + (pg + u) * CACHE_PAGE + 8 * h + 2 * t4;
-            if (key >= n) x[0] = x[2] = -INFINITY;
-            if (key + 1 >= n) x[1] = x[3] = -INFINITY;
+            x[0] = (x[0] + y[0]) * f0 + lg[u];
+            x[1] = (x[1] + y[1]) * f0 + lg[u];
+            x[2] = (x[2] + y[2]) * f1 + lg[u];
+            x[3] = (x[3] + y[3]) * f1 + lg[u];
+            if (cut) {
+              const int key = key0 + (pg + u) * CACHE_PAGE + 8 * h + 2 * t4;
+              if (key >= n) x[0] = x[2] = -INFINITY;
+              if (key + 1 >= n) x[1] = x[3] = -INFINITY;
+            }
             top[0] = fmaxf(top[0], fmaxf(x[0], x[1]));
             top[1] = fmaxf(top[1], fmaxf(x[2], x[3]));
           }
@@ -565,16 +626,14 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
       load_q(qf);
       float cv = 1.f;
       if (n > 0) {
-        const int page = c.page(s, 0);
-        const float f = page >= 0 ? c.scales[(head_block + page) * 2 + 1] * code_unit<FMT>() : 0.f;
+        const int first = c.page(use.s, 0);
+        const float f = first >= 0 ? c.scales[(((size_t)a.layer * c.kv + kvh) * c.n_pages + first) * 2 + 1] * code_unit<FMT>() : 0.f;
         if (f > 0.f) cv = std::is_same<T, bf16>::value ? f : fmaxf(f, 3.0517578125e-5f);   // (float16 weights w' / c stay below 2^15)
       }
       const float lgc = __log2f(cv), invc = __fdividef(1.f, cv);
+#pragma unroll 1
       for (; tile < tile1; ++tile) {
-        cp_async_wait<ST - 2>();
-        __syncthreads();
-        issue(tile + ST - 1);
-        const uint8_t* st = smem + (tile % ST) * STAGE;
+        const uint8_t* st = step(true);
         const int nt = tile - cached;
         unsigned long long vis[2];
 #pragma unroll
@@ -653,38 +712,33 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
         }
       }
     }
-    cp_async_wait<0>();
-    __syncthreads();
 
     // ---- the key groups' sums through shared memory: [kg][row][D] and (max, sum)
-    float* so = reinterpret_cast<float*>(smem);
+    float* so = reinterpret_cast<float*>(smem + ST * STAGE);
     float* sm = so + KG * MT * D;
+    __syncthreads();                             // (the last unit's sums have been read)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
       l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
+      if (!live[e]) continue;
       const int r = rg * 16 + g + 8 * e;
-      if (t4 == 0) {
-        sm[(kg * MT + r) * 2] = m[e];
-        sm[(kg * MT + r) * 2 + 1] = l[e];
-      }
+      if (t4 == 0) *reinterpret_cast<float2*>(sm + (kg * MT + r) * 2) = make_float2(m[e], l[e]);
 #pragma unroll
-      for (int i = 0; i < DT; ++i) *reinterpret_cast<float2*>(so + (kg * MT + r) * D + 8 * i + 2 * t4) = make_float2(o[i][2 * e], o[i][2 * e + 1]);
+      for (int i = 0; i < DT; ++i) *reinterpret_cast<float2*>(so + (kg * MT + r) * D + ((8 * i + 2 * t4) ^ ((r & 3) << 3))) = make_float2(o[i][2 * e], o[i][2 * e + 1]);
     }
     __syncthreads();
-    const bool whole = tile0 == 0 && tile1 == tiles;
-    const int unit = (b * pl.nrt + rt) * c.kv + kvh;
-    // a row's D values by D / 4 threads; `parts` sums behind one another, weighed by their maxima
+    const bool whole = tile0 == 0 && tile1 == use.tiles;
+    const int rows = min(MT, R * G - rtile * MT);   // rows of the tile that exist
     auto finish = [&](int r, int d, float top, float sum, float4 v) {
       const int mm = rtile * MT + r, i = mm / G, h = kvh * G + mm % G;
-      if (i >= R) return;
       const float f = sum > 0.f || sum != sum ? 1.f / sum : 0.f;      // (a sum that is NaN makes the row NaN)
-      uint2 w = make_uint2(pack2<T>(v.x * f, v.y * f), pack2<T>(v.z * f, v.w * f));
+      const uint2 w = make_uint2(pack2<T>(v.x * f, v.y * f), pack2<T>(v.z * f, v.w * f));
       const size_t row = (size_t)(r0 + i) * a.H + h;
       *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + row * D + d) = w;
       if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.693147180559945f;
     };
-    for (int x = tid; x < MT * D / 4; x += CAM_THREADS) {
+    for (int x = tid; x < rows * (D / 4); x += CAM_THREADS) {
       const int r = x / (D / 4), d = x % (D / 4) * 4;
       float top = -INFINITY;
 #pragma unroll
@@ -694,9 +748,10 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < KG; ++k) {
-        const float f = ex2(sm[(k * MT + r) * 2] - ref);
-        const float4 y = *reinterpret_cast<const float4*>(so + (k * MT + r) * D + d);
-        sum += f * sm[(k * MT + r) * 2 + 1];
+        const float2 ml = *reinterpret_cast<const float2*>(sm + (k * MT + r) * 2);
+        const float f = ex2(ml.x - ref);
+        const float4 y = *reinterpret_cast<const float4*>(so + (k * MT + r) * D + (d ^ ((r & 3) << 3)));
+        sum += f * ml.y;
         v.x += f * y.x;
         v.y += f * y.y;
         v.z += f * y.z;
@@ -705,32 +760,30 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
       if (whole) {
         finish(r, d, top, sum, v);
       } else {
-        float* out = pl.part + ((size_t)blockIdx.x * 2 + (at == run0 ? 0 : 1)) * (MT * (D + 2));
+        float* out = pl.part + ((size_t)blockIdx.x * 2 + (run0 > use.unit0 + CAM_UNIT ? 0 : 1)) * (MT * (D + 2));
         *reinterpret_cast<float4*>(out + r * D + d) = v;
-        if (d == 0) {
-          out[MT * D + 2 * r] = top;
-          out[MT * D + 2 * r + 1] = sum;
-        }
+        if (d == 0) *reinterpret_cast<float2*>(out + MT * D + 2 * r) = make_float2(top, sum);
       }
     }
     if (!whole) {
-      const long long c0 = owner(unit0), c1 = owner(unit0 + tiles - 1);
+      const int c0 = deal.owner(use.unit0 + CAM_UNIT), c1 = deal.owner(use.unit0 + CAM_UNIT + use.tiles - 1);
       __threadfence();
       __syncthreads();
       if (tid == 0) {
-        const int before = atomicAdd(pl.arrive + unit, 1);
-        last = before == (int)(c1 - c0);
-        if (last) pl.arrive[unit] = 0;
+        int* arrive = pl.arrive + ((size_t)use.b * pl.nrt + use.rt) * c.kv + kvh;
+        last = atomicAdd(arrive, 1) == c1 - c0;
+        if (last) *arrive = 0;
       }
       __syncthreads();
       if (last) {
         __threadfence();
-        for (int x = tid; x < MT * D / 4; x += CAM_THREADS) {
+        for (int x = tid; x < rows * (D / 4); x += CAM_THREADS) {
           const int r = x / (D / 4), d = x % (D / 4) * 4;
           float top = -INFINITY, sum = 0.f;
           float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (long long k = c0; k <= c1; ++k) {
-            const float* in = pl.part + ((size_t)k * 2 + (run_begin(k) < unit0 ? 1 : 0)) * (MT * (D + 2));
+#pragma unroll 4
+          for (int k = c0; k <= c1; ++k) {       // (the first of them has it as a unit that its run begins with or reaches, the others begin inside it)
+            const float* in = pl.part + ((size_t)k * 2 + (k == c0 ? 1 : 0)) * (MT * (D + 2));
             const float2 ml = __ldcg(reinterpret_cast<const float2*>(in + MT * D + 2 * r));
             const float4 y = __ldcg(reinterpret_cast<const float4*>(in + r * D + d));
             const float now = fmaxf(top, ml.x), ref = now == -INFINITY ? 0.f : now;
@@ -746,8 +799,8 @@ __global__ void __launch_bounds__(CAM_THREADS, RG == 4 ? 1 : 2) cache_attention_
         }
       }
     }
-    at += tile1 - tile0;
   }
+  cp_async_wait<0>();
 }
 
 }  // namespace spec
