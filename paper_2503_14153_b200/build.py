@@ -11,7 +11,7 @@ _SHARED = ["common.cuh", os.path.join("..", "..", "include", "spec_decode.h")]
 SOURCES = {
     "spec_api.cu": ["kernels_simple.cuh", "gemm_stream.cuh", "gemm_cluster.cuh", "gemm_glu.cuh", "gemm_pair.cuh", "glue_tc.cuh", "attention_tc.cuh",
                     "attention_umma.cuh", "labels.cuh"],
-    "cache_api.cu": ["cache_common.cuh", "cache_rows.cuh", "cache_pages.cuh", "cache_attention.cuh"],
+    "cache_api.cu": ["cache_common.cuh", "cache_rows.cuh", "cache_pages.cuh", "cache_attention.cuh", "cache_umma.cuh"],
 }
 
 

@@ -7,6 +7,7 @@
 #include "cache_common.cuh"
 #include "cache_pages.cuh"
 #include "cache_rows.cuh"
+#include "cache_umma.cuh"
 
 namespace spec {
 void set_last_error(const char* text) noexcept;   // spec_api.cu
@@ -63,30 +64,36 @@ template <typename F> auto by_shape(const spec_cache* c, F f) {
   return c->format == SPEC_CACHE_INT8 ? f(Int<64>{}, Int<CACHE_INT8>{}) : f(Int<64>{}, Int<CACHE_E4M3>{});
 }
 
-// Row groups of 16 (sequence row, head) rows that a CTA of the tensor-core kernel has: as few as hold all rows of a (sequence, kv head), at most 4.
-int row_groups(long long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
 struct AttnShape {
-  int rg, mt;
-  long long tiles, pairs;       // row tiles of a sequence, (sequence, row tile) pairs of a launch at most
+  int mt;                       // (row, head) rows of a row tile: 16, 32 on mma.sync, 64, 128, 256 on tcgen05
+  int limit;                    // (sequence, row tile) pairs of a launch
+  long long tiles, pairs;       // row tiles of a sequence; pairs of a launch at most
   size_t arrive_bytes, bytes;
 };
 AttnShape attn_shape(const spec_cache* c, int n_heads, int batch, int max_rows) {
   AttnShape s;
   const long long rows = (long long)max_rows * (n_heads / c->n_kv_heads);
-  s.rg = row_groups(rows);
-  s.mt = 16 * s.rg;
+  s.mt = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  s.limit = s.mt <= 32 ? CAM_PAIRS : CU_PAIRS;
   s.tiles = (rows + s.mt - 1) / s.mt;
-  s.pairs = s.tiles * batch < CAM_PAIRS ? s.tiles * batch : CAM_PAIRS;
+  s.pairs = s.tiles * batch < s.limit ? s.tiles * batch : s.limit;
   s.arrive_bytes = ((size_t)s.pairs * c->n_kv_heads * 4 + 255) / 256 * 256;
   s.bytes = s.arrive_bytes + (size_t)CAM_SMS * 2 * s.mt * (c->head_dim + 2) * 4;
   return s;
 }
-template <typename T, int D, int FMT, int RG> int launch_mma(const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
-  auto kernel = cache_attention_mma<T, D, FMT, RG>;
-  const size_t smem = cam_smem(D);
+template <typename K> int launch_attn(K kernel, int threads, size_t smem, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return launched("spec_cache_attention: shared memory");
-  kernel<<<CAM_SMS, CAM_THREADS, smem, st>>>(a, pl);
+  kernel<<<CAM_SMS, threads, smem, st>>>(a, pl);
   return launched("spec_cache_attention");
+}
+template <typename T, int D, int FMT> int launch_attn(int mt, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
+  switch (mt) {
+    case 16: return launch_attn(cache_attention_mma<T, D, FMT, 1>, CAM_THREADS, cam_smem(D), a, pl, st);
+    case 32: return launch_attn(cache_attention_mma<T, D, FMT, 2>, CAM_THREADS, cam_smem(D), a, pl, st);
+    case 64: return launch_attn(cache_attention_umma<T, D, FMT, 64>, CU_THREADS, cu_smem(D, 64), a, pl, st);
+    case 128: return launch_attn(cache_attention_umma<T, D, FMT, 128>, CU_THREADS, cu_smem(D, 128), a, pl, st);
+    default: return launch_attn(cache_attention_umma<T, D, FMT, 256>, CU_THREADS, cu_smem(D, 256), a, pl, st);
+  }
 }
 unsigned copy_blocks(size_t units) {
   const size_t blocks = (units + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32), most = 148 * 8;
@@ -238,7 +245,7 @@ int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void
   if (r->rows == 0 || r->batch == 0) return SPEC_OK;
   if (!r->q || !r->k || !r->v || !r->out) return fail(SPEC_E_BADARG, "spec_cache_attention: null pointer");
   if (r->rows < 0 || r->batch < 0 || r->batch > 65535 || r->n_heads < 1 || r->n_heads % c->n_kv_heads || r->layer < 0 || r->layer >= c->n_layers || (!r->row_offsets && r->rows % r->batch) || r->max_rows < 1 ||
-      (!r->row_offsets && r->max_rows < r->rows / r->batch) || r->mask_words < 0 || (r->mask && r->mask_words < 1) || (long long)r->rows * r->n_heads > 0x7fffffffLL)
+      (!r->row_offsets && r->max_rows < r->rows / r->batch) || r->mask_words < 0 || (r->mask && r->mask_words < 1) || !(r->scale > 0.f && r->scale <= 3.4e38f) || (long long)r->rows * r->n_heads > 0x7fffffffLL)
     return fail(SPEC_E_BADARG, "spec_cache_attention: unsupported sizes (%d rows, batch %d, %d heads over %d, layer %d of %d, max_rows %d)", r->rows, r->batch, r->n_heads, c->n_kv_heads, r->layer, c->n_layers, r->max_rows);
   if (!known_type(r->type)) return fail(SPEC_E_BADARG, "spec_cache_attention: unknown type");
   if (r->type != SPEC_TYPE_F32) {
@@ -257,9 +264,9 @@ int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void
     by_shape(c, [&](auto d, auto f) { cache_attention_simple<float, decltype(d)::value, decltype(f)::value><<<grid, CAS_THREADS, 0, st>>>(a); });
     return launched("spec_cache_attention");
   }
-  // launches of at most CAM_PAIRS (sequence, row tile) pairs
+  // launches of at most sh.limit (sequence, row tile) pairs
   const int tiles = (int)(((long long)max_rows * (r->n_heads / c->n_kv_heads) + sh.mt - 1) / sh.mt);
-  const int nrt = tiles < CAM_PAIRS ? tiles : CAM_PAIRS, nb = CAM_PAIRS / nrt;
+  const int nrt = tiles < sh.limit ? tiles : sh.limit, nb = sh.limit / nrt;
   for (int b0 = 0; b0 < r->batch; b0 += nb)
     for (int rt0 = 0; rt0 < tiles; rt0 += nrt) {
       const CamPlan pl{b0, r->batch - b0 < nb ? r->batch - b0 : nb, rt0, tiles - rt0 < nrt ? tiles - rt0 : nrt, static_cast<int*>(scratch),
@@ -268,7 +275,7 @@ int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void
         auto go = [&](auto t) {
           typedef decltype(t) T;
           constexpr int D = decltype(d)::value, F = decltype(f)::value;
-          return sh.rg == 1 ? launch_mma<T, D, F, 1>(a, pl, st) : sh.rg == 2 ? launch_mma<T, D, F, 2>(a, pl, st) : launch_mma<T, D, F, 4>(a, pl, st);
+          return launch_attn<T, D, F>(sh.mt, a, pl, st);
         };
         return r->type == SPEC_TYPE_BF16 ? go(bf16{}) : go(f16{});
       });

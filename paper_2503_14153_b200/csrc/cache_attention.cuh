@@ -270,37 +270,32 @@ struct CamCursor {
   long long unit0;                       // first slot of the unit
 };
 
-template <typename T, int D, int FMT, int RG>
-__global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnArgs a, CamPlan pl) {
-  constexpr int KG = CAM_WARPS / RG, MT = 16 * RG, ST = CAM_STAGES, NP = CAM_PAGES / KG;
-  constexpr int DC = D / 16, DT = D / 8, STAGE = cam_stage_bytes(D), BLOCK = CACHE_PAGE * D;
-  constexpr bool ALONE = RG == 1;                // a warp uses only the pages it fetched itself
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int pre[CAM_PAIRS + 1];
-  __shared__ int scan[CAM_WARPS];
-  __shared__ int last;
-  const CacheView& c = a.c;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-  const int rg = warp % RG, kg = warp / RG;
-  const int G = a.H / c.kv, pairs = pl.nb * pl.nrt;
+// The list of units as a CTA sees it. MT: rows of a row tile; NEW: rows of the pass a tile; pre: prefix sums over the (sequence, row tile) pairs, in shared memory.
+template <int MT, int NEW> struct CamList {
+  const CacheAttnArgs& a;
+  const CamPlan& pl;
+  const int* pre;
+  CamDeal deal;
+  long long run0, run1;
 
-  // ---- the list of units: slots of every (sequence, row tile), one kv head; prefix sums
-  auto fill = [&](CamCursor& u) {                // the numbers of unit (b, rt)
-    const int b = pl.b0 + u.b, m0 = (pl.rt0 + u.rt) * MT;
+  __device__ __forceinline__ static void fill(const CacheAttnArgs& a, const CamPlan& pl, CamCursor& u) {   // the numbers of unit (b, rt)
+    const int b = pl.b0 + u.b, m0 = (pl.rt0 + u.rt) * MT, G = a.H / a.c.kv;
     u.r0 = rows_begin(a.row_offsets, b, a.rows, a.batch);
     u.R = max(0, rows_begin(a.row_offsets, b + 1, a.rows, a.batch) - u.r0);
     const int left = u.R * G - m0;
     u.cached = u.tiles = u.n = 0;
     u.s = -1;
     if (left <= 0) return;
-    u.s = c.sequence(a.seqs, b);
-    u.n = u.s < 0 ? 0 : c.len(u.s);
+    u.s = a.c.sequence(a.seqs, b);
+    u.n = u.s < 0 ? 0 : a.c.len(u.s);
     u.cached = (u.n + CAM_TILE - 1) / CAM_TILE;
     const int seen = a.mask ? u.R : min(u.R, (m0 + min(left, MT) - 1) / G + 1);
-    u.tiles = u.cached + (seen + CAM_NEW - 1) / CAM_NEW;
-  };
-  {
-    const int each = (pairs + CAM_THREADS - 1) / CAM_THREADS;
+    u.tiles = u.cached + (seen + NEW - 1) / NEW;
+  }
+  // Fills `pre` (all threads of the block; scan: an int a warp); false if this CTA has nothing to do.
+  template <int THREADS> __device__ __forceinline__ bool make(int* table, int* scan) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, pairs = pl.nb * pl.nrt;
+    const int each = (pairs + THREADS - 1) / THREADS;
     int mine = 0;
     for (int i = 0; i < each; ++i) {
       const int p = tid * each + i;
@@ -308,9 +303,9 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
         CamCursor u;
         u.b = p / pl.nrt;
         u.rt = p - u.b * pl.nrt;
-        fill(u);
-        pre[p] = u.tiles ? u.tiles + CAM_UNIT : 0;
-        mine += pre[p];
+        fill(a, pl, u);
+        table[p] = u.tiles ? u.tiles + CAM_UNIT : 0;
+        mine += table[p];
       }
     }
     int x = mine;
@@ -326,35 +321,36 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
     for (int i = 0; i < each; ++i) {
       const int p = tid * each + i;
       if (p < pairs) {
-        const int w = pre[p];
-        pre[p] = at;
+        const int w = table[p];
+        table[p] = at;
         at += w;
-        if (p == pairs - 1) pre[pairs] = at;
+        if (p == pairs - 1) table[pairs] = at;
       }
     }
     __syncthreads();
+    pre = table;
+    deal.total = (long long)table[pairs] * a.c.kv;
+    deal.ctas = (int)min((long long)gridDim.x, deal.total);
+    deal.small = deal.total < (1 << 23);
+    if ((int)blockIdx.x >= deal.ctas) return false;
+    run0 = deal.begin(blockIdx.x);
+    run1 = deal.begin(blockIdx.x + 1);
+    return true;
   }
-  CamDeal deal;
-  deal.total = (long long)pre[pairs] * c.kv;
-  deal.ctas = (int)min((long long)gridDim.x, deal.total);
-  deal.small = deal.total < (1 << 23);
-  if ((int)blockIdx.x >= deal.ctas) return;
-  const long long run0 = deal.begin(blockIdx.x), run1 = deal.begin(blockIdx.x + 1);
-
-  // the first tile of the run, or the next one; false when the run is over
-  auto enter = [&](CamCursor& u, long long at) {   // at: a slot of the unit, u.unit0 its first
-    fill(u);
+  __device__ __forceinline__ void enter(CamCursor& u, long long at) const {   // at: a slot of the unit, u.unit0 its first
+    fill(a, pl, u);
     u.tile = max(0, (int)(at - u.unit0) - CAM_UNIT);
     u.tile1 = (int)min((long long)u.tiles, run1 - u.unit0 - CAM_UNIT);
-  };
-  auto next_unit = [&](CamCursor& u) {
+  }
+  // the next unit of the run that has tiles in it; false when the run is over
+  __device__ __forceinline__ bool next(CamCursor& u) const {
     long long at = u.unit0 + u.tiles + CAM_UNIT;
     do {
       if (at >= run1) return false;
       do {
         if (++u.rt == pl.nrt) {
           u.rt = 0;
-          if (++u.kvh == c.kv) {
+          if (++u.kvh == a.c.kv) {
             u.kvh = 0;
             ++u.b;
           }
@@ -365,29 +361,93 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
       at += u.tiles + CAM_UNIT;
     } while (u.tile >= u.tile1);
     return true;
-  };
-  CamCursor use;
-  {
+  }
+  __device__ __forceinline__ bool first(CamCursor& u) const {
     int lo = 0, hi = pl.nb;                      // the last sequence whose units begin at or before the run (one without units begins where the next one does)
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if ((long long)pre[mid * pl.nrt] * c.kv <= run0) lo = mid; else hi = mid;
+      if ((long long)pre[mid * pl.nrt] * a.c.kv <= run0) lo = mid; else hi = mid;
     }
-    use.b = lo;
+    u.b = lo;
     const int p0 = lo * pl.nrt, w = pre[p0 + pl.nrt] - pre[p0];
-    const long long in = run0 - (long long)pre[p0] * c.kv;
-    use.kvh = deal.small ? (int)((uint32_t)in / (uint32_t)w) : (int)(in / w);
-    const int r = (int)(in - (long long)use.kvh * w) + pre[p0];
+    const long long in = run0 - (long long)pre[p0] * a.c.kv;
+    u.kvh = deal.small ? (int)((uint32_t)in / (uint32_t)w) : (int)(in / w);
+    const int r = (int)(in - (long long)u.kvh * w) + pre[p0];
     lo = p0, hi = p0 + pl.nrt;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (pre[mid] <= r) lo = mid; else hi = mid;
     }
-    use.rt = lo - p0;
-    use.unit0 = run0 - (r - pre[lo]);
-    enter(use, run0);
-    if (use.tile >= use.tile1 && !next_unit(use)) return;
+    u.rt = lo - p0;
+    u.unit0 = run0 - (r - pre[lo]);
+    enter(u, run0);
+    return u.tile < u.tile1 || next(u);
   }
+  // ---- parts of a unit that is cut: where this CTA leaves its own, and who has the others. The first of a unit's CTAs reaches its first tile from before (slot 1), the others begin
+  // inside it (slot 0); so a CTA that ends one unit and begins another has a slot for each.
+  __device__ __forceinline__ float* part(const CamCursor& u, int D) const {
+    return pl.part + ((size_t)blockIdx.x * 2 + (run0 > u.unit0 + CAM_UNIT ? 0 : 1)) * ((size_t)MT * (D + 2));
+  }
+  __device__ __forceinline__ const float* part_of(int cta, int c0, int D) const { return pl.part + ((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * ((size_t)MT * (D + 2)); }
+  __device__ __forceinline__ int first_cta(const CamCursor& u) const { return deal.owner(u.unit0 + CAM_UNIT); }
+  __device__ __forceinline__ int last_cta(const CamCursor& u) const { return deal.owner(u.unit0 + CAM_UNIT + u.tiles - 1); }
+  __device__ __forceinline__ int* arrive(const CamCursor& u) const { return pl.arrive + ((size_t)u.b * pl.nrt + u.rt) * a.c.kv + u.kvh; }
+};
+
+// A finished row's values d .. d + 3 and, with d = 0, its lse. m: row of the unit's row tile `rtile`.
+template <typename T, int D, int MT>
+__device__ __forceinline__ void cam_finish(const CacheAttnArgs& a, int r0, int rtile, int kvh, int r, int d, float top, float sum, float4 v) {
+  const int G = a.H / a.c.kv, mm = rtile * MT + r, i = mm / G, h = kvh * G + mm % G;
+  const float f = sum > 0.f || sum != sum ? 1.f / sum : 0.f;      // (a sum that is NaN makes the row NaN)
+  const size_t row = (size_t)(r0 + i) * a.H + h;
+  *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + row * D + d) = make_uint2(pack2<T>(v.x * f, v.y * f), pack2<T>(v.z * f, v.w * f));
+  if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.693147180559945f;
+}
+
+// The parts of a unit, all left by now, added in the order of their CTAs by `threads` threads.
+template <typename T, int D, int MT, typename L>
+__device__ __forceinline__ void cam_join(const L& list, const CamCursor& u, int rows, int c0, int c1, int tid, int threads) {
+  __threadfence();
+  for (int x = tid; x < rows * (D / 4); x += threads) {
+    const int r = x / (D / 4), d = x % (D / 4) * 4;
+    float top = -INFINITY, sum = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int k = c0; k <= c1; ++k) {
+      const float* in = list.part_of(k, c0, D);
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(in + MT * D + 2 * r));
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(in + r * D + d));
+      const float now = fmaxf(top, ml.x), ref = now == -INFINITY ? 0.f : now;
+      const float f = ex2(top - ref), h = ex2(ml.x - ref);
+      sum = f * sum + h * ml.y;
+      v.x = f * v.x + h * y.x;
+      v.y = f * v.y + h * y.y;
+      v.z = f * v.z + h * y.z;
+      v.w = f * v.w + h * y.w;
+      top = now;
+    }
+    cam_finish<T, D, MT>(list.a, u.r0, list.pl.rt0 + u.rt, u.kvh, r, d, top, sum, v);
+  }
+}
+
+template <typename T, int D, int FMT, int RG>
+__global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnArgs a, CamPlan pl) {
+  constexpr int KG = CAM_WARPS / RG, MT = 16 * RG, ST = CAM_STAGES, NP = CAM_PAGES / KG;
+  constexpr int DC = D / 16, DT = D / 8, STAGE = cam_stage_bytes(D), BLOCK = CACHE_PAGE * D;
+  constexpr bool ALONE = RG == 1;                // a warp uses only the pages it fetched itself
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int pre[CAM_PAIRS + 1];
+  __shared__ int scan[CAM_WARPS];
+  __shared__ int last;
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+  const int rg = warp % RG, kg = warp / RG;
+  const int G = a.H / c.kv;
+
+  CamList<MT, CAM_NEW> list{a, pl};
+  if (!list.template make<CAM_THREADS>(pre, scan)) return;
+  CamCursor use;
+  if (!list.first(use)) return;
   CamCursor get = use;
   bool more = true;                              // `get` stands at a tile
 
@@ -427,7 +487,7 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
         }
       }
       if (++slot == ST) slot = 0;
-      if (++get.tile == get.tile1) more = next_unit(get);
+      if (++get.tile == get.tile1) more = list.next(get);
       if (more) page = page_of(get);
     }
     cp_async_commit();
@@ -451,7 +511,7 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
     return st;
   };
 
-  for (bool go = true; go; go = next_unit(use)) {
+  for (bool go = true; go; go = list.next(use)) {
     const int R = use.R, n = use.n, kvh = use.kvh, r0 = use.r0, cached = use.cached, tile1 = use.tile1, tile0 = use.tile, rtile = pl.rt0 + use.rt;
 
     // ---- the warp's 16 rows of q: lane (g, t) holds dims 16 i + 4 t .. + 3 of rows g and g + 8
@@ -730,14 +790,6 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
     __syncthreads();
     const bool whole = tile0 == 0 && tile1 == use.tiles;
     const int rows = min(MT, R * G - rtile * MT);   // rows of the tile that exist
-    auto finish = [&](int r, int d, float top, float sum, float4 v) {
-      const int mm = rtile * MT + r, i = mm / G, h = kvh * G + mm % G;
-      const float f = sum > 0.f || sum != sum ? 1.f / sum : 0.f;      // (a sum that is NaN makes the row NaN)
-      const uint2 w = make_uint2(pack2<T>(v.x * f, v.y * f), pack2<T>(v.z * f, v.w * f));
-      const size_t row = (size_t)(r0 + i) * a.H + h;
-      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + row * D + d) = w;
-      if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.693147180559945f;
-    };
     for (int x = tid; x < rows * (D / 4); x += CAM_THREADS) {
       const int r = x / (D / 4), d = x % (D / 4) * 4;
       float top = -INFINITY;
@@ -758,46 +810,24 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
         v.w += f * y.w;
       }
       if (whole) {
-        finish(r, d, top, sum, v);
+        cam_finish<T, D, MT>(a, r0, rtile, kvh, r, d, top, sum, v);
       } else {
-        float* out = pl.part + ((size_t)blockIdx.x * 2 + (run0 > use.unit0 + CAM_UNIT ? 0 : 1)) * (MT * (D + 2));
+        float* out = list.part(use, D);
         *reinterpret_cast<float4*>(out + r * D + d) = v;
         if (d == 0) *reinterpret_cast<float2*>(out + MT * D + 2 * r) = make_float2(top, sum);
       }
     }
     if (!whole) {
-      const int c0 = deal.owner(use.unit0 + CAM_UNIT), c1 = deal.owner(use.unit0 + CAM_UNIT + use.tiles - 1);
+      const int c0 = list.first_cta(use), c1 = list.last_cta(use);
       __threadfence();
       __syncthreads();
       if (tid == 0) {
-        int* arrive = pl.arrive + ((size_t)use.b * pl.nrt + use.rt) * c.kv + kvh;
+        int* arrive = list.arrive(use);
         last = atomicAdd(arrive, 1) == c1 - c0;
         if (last) *arrive = 0;
       }
       __syncthreads();
-      if (last) {
-        __threadfence();
-        for (int x = tid; x < rows * (D / 4); x += CAM_THREADS) {
-          const int r = x / (D / 4), d = x % (D / 4) * 4;
-          float top = -INFINITY, sum = 0.f;
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int k = c0; k <= c1; ++k) {       // (the first of them has it as a unit that its run begins with or reaches, the others begin inside it)
-            const float* in = pl.part + ((size_t)k * 2 + (k == c0 ? 1 : 0)) * (MT * (D + 2));
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(in + MT * D + 2 * r));
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(in + r * D + d));
-            const float now = fmaxf(top, ml.x), ref = now == -INFINITY ? 0.f : now;
-            const float f = ex2(top - ref), h = ex2(ml.x - ref);
-            sum = f * sum + h * ml.y;
-            v.x = f * v.x + h * y.x;
-            v.y = f * v.y + h * y.y;
-            v.z = f * v.z + h * y.z;
-            v.w = f * v.w + h * y.w;
-            top = now;
-          }
-          finish(r, d, top, sum, v);
-        }
-      }
+      if (last) cam_join<T, D, MT>(list, use, rows, c0, c1, tid, CAM_THREADS);
     }
   }
   cp_async_wait<0>();

@@ -1,0 +1,563 @@
+// Attention over the 8-bit paged cache on the 5th-generation tensor cores, for passes whose rows fill them: trees of many nodes, groups of query
+// heads that share a kv head, prompts. The mathematics is that of cache_attention.cuh (the page's scale of V in the exponent); what differs is who does what.
+//
+// A CTA has ROWS = 64, 128 or 256 (row, head) rows of one (sequence, kv head) and takes its run of tiles of 128 keys:
+//   producer warp     brings a tile's pages (K and V of a page are one block) with bulk copies, 8 a tile, one a lane;
+//   4 converter warps turn codes into operands of the query's type: a 16-byte row of a core matrix (16 dims of a token, 16 tokens of a dim) becomes two 16-byte
+//                     chunks of a 128-byte-swizzled K-major tile, so K [128 keys][D] and V^T [D][128 keys] need no transpose; rows of the pass are copied (V as it is: MN-major);
+//   one thread        issues S = Q K^T and O += P V;
+//   8 softmax warps   in two groups, a thread a row: S out of tensor memory, weights back into the same columns as the A operand of P V.
+// With 64 rows the rows are given twice to the 128-row MMA, rows 64.. taking care of the second half of every tile's keys (P is block-diagonal), so that all four
+// SM quarters work; with 64 and 128 the groups take alternate tiles, each with its own S and O; with 256 each group has 128 rows and takes all tiles, so that a tile is converted once for 256 rows.
+// The running reference is raised only when a tile's maximum exceeds it by more than 2^8; a group's O row is then rescaled in place.
+#pragma once
+#include "cache_attention.cuh"
+
+namespace spec {
+
+constexpr int CU_SOFT = 8, CU_CONV = 4;                       // softmax and converter warps
+constexpr int CU_WARPS = CU_SOFT + CU_CONV + 2, CU_THREADS = 32 * CU_WARPS;
+constexpr int CU_PAIRS = 160;                                 // (sequence, row tile) pairs a launch can deal
+constexpr int CU_NEW = 128;                                   // rows of the pass a tile
+constexpr float CU_RAISE = 8.f;
+
+__host__ __device__ constexpr int cu_code_stages(int ROWS) { return ROWS == 256 ? 1 : 2; }
+__host__ __device__ constexpr size_t cu_smem(int D, int ROWS) {
+  return 1024 + (size_t)(ROWS == 256 ? 2 : 1) * 128 * D * 2 /*Q*/ + 2 * (size_t)(2 * 128 * D * 2) /*K, V*/ + (size_t)cu_code_stages(ROWS) * 256 * D /*codes*/;
+}
+
+// D[tmem] (+)= A[tmem] * B[smem]
+__device__ __forceinline__ void tc_mma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+template <typename T, int D, int FMT, int ROWS>
+__global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnArgs a, CamPlan pl) {
+  constexpr int CS = cu_code_stages(ROWS), BLOCK = CACHE_PAGE * D, OPER = 128 * D * 2;   // OPER: bytes of one operand tile (Q, K or V)
+  constexpr int NQ = ROWS == 256 ? 2 : 1;
+  constexpr bool ALT = ROWS != 256;                            // the groups take alternate tiles
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(16) uint64_t bars[22];
+  __shared__ float4 consts[4][CAM_PAGES];                      // a page's scale of K, log2 and reciprocal of its scale of V; by cached tile
+  __shared__ float2 xm[64];
+  __shared__ int pre[CU_PAIRS + 1], scan[CU_WARPS], odd[8], last;
+  __shared__ uint32_t tmem_slot;
+  const uint32_t raw = smem_u32(smem_raw);
+  uint8_t* q_s = smem_raw + (((raw + 1023u) & ~1023u) - raw);
+  uint8_t* kv_s = q_s + NQ * OPER;                             // [2 stages][K, V]
+  uint8_t* code_s = kv_s + 4 * OPER;
+  uint64_t *code_full = bars, *code_empty = bars + 2, *k_full = bars + 4, *k_empty = bars + 6, *v_full = bars + 8, *v_empty = bars + 10, *s_full = bars + 12, *p_full = bars + 14, *q_full = bars + 16,
+           *q_empty = bars + 17, *o_full = bars + 18;
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.H / c.kv;
+  int* status = c.status;
+
+  CamList<ROWS, CU_NEW> list{a, pl};
+  if (!list.template make<CU_THREADS>(pre, scan)) return;      // (all threads of the CTA agree, before anything is allocated)
+  CamCursor u;
+  if (!list.first(u)) return;
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(code_full + i, 1);
+      mbar_init(code_empty + i, CU_CONV);
+      mbar_init(k_full + i, CU_CONV);
+      mbar_init(k_empty + i, 1);
+      mbar_init(v_full + i, CU_CONV);
+      mbar_init(v_empty + i, 1);
+      mbar_init(s_full + i, 1);
+      mbar_init(p_full + i, 4);
+    }
+    for (int i = 0; i < 8; ++i) odd[i] = 0;
+    mbar_init(q_full, CU_CONV);
+    mbar_init(q_empty, ALT ? 1 + CU_SOFT : 1);
+    mbar_init(o_full, 1);
+    mbar_fence_init();
+  }
+  if (warp == CU_SOFT + CU_CONV + 1) {
+    tmem_alloc(&tmem_slot, 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  const size_t layer_heads = (size_t)a.layer * c.kv;
+
+  if (warp == CU_SOFT + CU_CONV) {
+    // ---- producer: the pages of cached tiles. Lane p < 8 has page p of a tile; its number and scales are asked for a tile ahead.
+    int C = 0;
+    bool go = true;
+    auto look = [&](const CamCursor& w, int tile, float2& sc) {
+      const int p = tile * CAM_PAGES + lane;
+      const int page = lane < CAM_PAGES && tile < min(w.tile1, w.cached) && p * CACHE_PAGE < w.n ? c.page(w.s, p) : -1;
+      sc = make_float2(0.f, 0.f);
+      if (page >= 0) sc = *reinterpret_cast<const float2*>(c.scales + ((layer_heads + w.kvh) * c.n_pages + page) * 2);
+      return page;
+    };
+    do {
+      float2 sc, sc_next;
+      int page = look(u, u.tile, sc);
+      for (int tile = u.tile; tile < min(u.tile1, u.cached) && go; ++tile, ++C) {
+        const int cs = C % CS;
+        const int page_next = look(u, tile + 1, sc_next);
+        if (C >= CS) go = mbar_wait(code_empty + cs, ((C / CS) - 1) & 1, status, 301);
+        if (!__all_sync(0xffffffffu, go)) { go = false; break; }
+        const float v = sc.y > 0.f ? sc.y * code_unit<FMT>() : 9.094947017729282e-13f;    // (a block of zeros: 2^-40 does not raise the reference)
+        if (lane < CAM_PAGES) consts[C & 3][lane] = make_float4(sc.x * code_unit<FMT>() * a.scale * 1.44269504088896f, __log2f(v), __fdividef(1.f, v), 0.f);
+        const uint32_t valid = __ballot_sync(0xffffffffu, page >= 0);
+        if (lane == 0) mbar_expect_tx(code_full + cs, __popc(valid) * 2 * BLOCK);
+        __syncwarp();
+        if (page >= 0) bulk_load_1d(code_s + (size_t)cs * 256 * D + lane * 2 * BLOCK, c.codes + ((layer_heads + u.kvh) * c.n_pages + page) * (2 * (size_t)BLOCK), 2 * BLOCK, code_full + cs);
+        page = page_next;
+        sc = sc_next;
+      }
+    } while (go && list.next(u));
+    // (copies still in flight: the last of each stage)
+    if (!go)
+      for (int x = max(0, C - CS); x < C; ++x) mbar_wait(code_full + x % CS, (x / CS) & 1, status, 302);
+  } else if (warp == CU_SOFT + CU_CONV + 1) {
+    // ---- MMA issuer
+    if (elect_one()) {
+      constexpr uint32_t fm = std::is_same<T, bf16>::value ? (1u << 7) | (1u << 10) : 0u;        // operand formats: bf16 or f16
+      constexpr uint32_t idesc_s = (1u << 4) | fm | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+      constexpr uint32_t idesc_o = (1u << 4) | fm | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+      const uint32_t q_addr = smem_u32(q_s);
+      int T0 = 0, U = 0;
+      bool go = true;
+      do {
+        const int nt = u.tile1 - u.tile;
+        auto mma_s = [&](int t, int x) {           // scores of tile t; x: S buffer and, with 256 rows, Q tile
+          const int st = (T0 + t) & 1;
+          if (t == 0 && x == (ALT ? (T0 & 1) : 0) && !mbar_wait(q_full, U & 1, status, 303)) return false;
+          if (!mbar_wait(k_full + st, ((T0 + t) >> 1) & 1, status, 304)) return false;
+          tc_fence_after();
+          const uint32_t k_addr = smem_u32(kv_s + st * 2 * OPER), qa = q_addr + (ALT ? 0 : x * OPER);
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j)
+            tc_mma_f16(tmem + x * 128, make_kmajor_sw128_desc(qa + (j >> 2) * 16384) + 2 * (j & 3), make_kmajor_sw128_desc(k_addr + (j >> 2) * 16384) + 2 * (j & 3), idesc_s, j > 0);
+          tc_commit(s_full + x);
+          if (ALT || x == 1) {
+            tc_commit(k_empty + st);
+            if (t == nt - 1) tc_commit(q_empty);
+          }
+          return true;
+        };
+        auto mma_o = [&](int t, int x, bool first) {
+          const int gt = T0 + t, st = gt & 1;
+          if (!mbar_wait(p_full + x, (ALT ? gt >> 1 : gt) & 1, status, 305) || !mbar_wait(v_full + st, (gt >> 1) & 1, status, 306)) return false;
+          tc_fence_after();
+          const uint32_t v_addr = smem_u32(kv_s + st * 2 * OPER + OPER);
+          const bool is_new = u.tile + t >= u.cached;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {             // 16 keys
+            const uint64_t bd = is_new ? make_sw128_desc(v_addr + j * 2048, 16384, 1024) : make_kmajor_sw128_desc(v_addr + (j >> 2) * (D * 128)) + 2 * (j & 3);
+            tc_mma_f16_ts(tmem + 256 + x * 128, tmem + x * 128 + j * 8, bd, is_new ? idesc_o | (1u << 16) : idesc_o, !first || j > 0);
+          }
+          if (ALT || x == 1) tc_commit(v_empty + st);
+          return true;
+        };
+        if constexpr (ALT) {
+          go = mma_s(0, T0 & 1) && (nt < 2 || mma_s(1, (T0 + 1) & 1));
+          for (int t = 0; t < nt && go; ++t) go = mma_o(t, (T0 + t) & 1, t < 2) && (t + 2 >= nt || mma_s(t + 2, (T0 + t) & 1));
+        } else {
+          go = mma_s(0, 0) && mma_s(0, 1);
+          for (int t = 0; t < nt && go; ++t) {
+            go = mma_o(t, 0, t == 0) && (t + 1 >= nt || mma_s(t + 1, 0));
+            go = go && mma_o(t, 1, t == 0) && (t + 1 >= nt || mma_s(t + 1, 1));
+          }
+        }
+        tc_commit(o_full);
+        T0 += nt;
+        ++U;
+      } while (go && list.next(u));
+      // (whatever was issued is through before the CTA gives its memory back)
+      if (!go) mbar_wait(o_full, (U - 1) & 1, status, 307);
+    }
+    __syncwarp();
+  } else if (warp >= CU_SOFT) {
+    // ---- converters
+    const int ct = tid - CU_SOFT * 32;
+    auto tell = [&](uint64_t* bar) {               // what this warp's threads wrote may be read by the tensor cores
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
+    int gt = 0, C = 0, U = 0;
+    bool go = true;
+    do {
+      const int rtile = pl.rt0 + u.rt;
+      // q: row r of the tile at row r (64 rows: and at r + 64), 16-byte chunk ch at chunk ch ^ (r % 8) of its 128 bytes
+      if (U > 0) go = mbar_wait(q_empty, (U - 1) & 1, status, 308);
+      if (!go) break;
+      for (int x = ct; x < NQ * 128 * (D / 8); x += CU_CONV * 32) {
+        const int r = x / (D / 8), ch = x % (D / 8), m = rtile * ROWS + (ROWS == 64 ? r & 63 : r), i = m / G;
+        const bool live = i < u.R;
+        const T* src = static_cast<const T*>(a.q) + (long long)(u.r0 + (live ? i : 0)) * a.q_row + (long long)(u.kvh * G + (live ? m - i * G : 0)) * a.q_head + ch * 8;
+        cp_async16(smem_u32(q_s) + (r >> 7) * OPER + (ch >> 3) * 16384 + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4), src, live ? 16 : 0);
+      }
+      cp_async_commit();
+      if (ct == 0) odd[(U + 4) & 7] = 0;    // (no unit that is still worked on: the roles are at most three apart)
+      bool q_told = false;
+      for (int tile = u.tile; tile < u.tile1; ++tile, ++gt) {
+        const int st = gt & 1;
+        uint8_t* k_s = kv_s + st * 2 * OPER;
+        uint8_t* v_s = k_s + OPER;
+        if (tile < u.cached) {
+          const int cs = C % CS;
+          go = mbar_wait(code_full + cs, (C / CS) & 1, status, 309) && (gt < 2 || mbar_wait(k_empty + st, ((gt >> 1) - 1) & 1, status, 310));
+          if (!go) break;
+          const uint4* codes = reinterpret_cast<const uint4*>(code_s + (size_t)cs * 256 * D);
+#pragma unroll 4
+          for (int it = 0; it < CAM_PAGES * D / (CU_CONV * 32); ++it) {
+            const int x = it * CU_CONV * 32 + ct, p = x / D, y = x % D;
+            const uint4 w = codes[p * (2 * D) + y];
+            const int ch = (y >> 3) % (D / 16), key = p * 16 + (y / (D / 2)) * 8 + (y & 7);
+            uint32_t o[8];
+            codes_to<FMT, T>(w.x, o[0], o[1]);
+            codes_to<FMT, T>(w.y, o[2], o[3]);
+            codes_to<FMT, T>(w.z, o[4], o[5]);
+            codes_to<FMT, T>(w.w, o[6], o[7]);
+            uint8_t* row = k_s + (ch >> 2) * 16384 + key * 128;
+            const int j = (ch & 3) * 2;
+            *reinterpret_cast<uint4*>(row + ((j ^ (key & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(row + (((j + 1) ^ (key & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+          }
+          if (!q_told) {
+            cp_async_wait<0>();
+            tell(q_full);
+            q_told = true;
+          }
+          tell(k_full + st);
+          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 311)) { go = false; break; }
+#pragma unroll 4
+          for (int it = 0; it < CAM_PAGES * D / (CU_CONV * 32); ++it) {
+            const int x = it * CU_CONV * 32 + ct, p = x / D, d = x % D;
+            const uint4 w = codes[p * (2 * D) + D + d];
+            uint32_t o[8];
+            codes_to<FMT, T>(w.x, o[0], o[1]);
+            codes_to<FMT, T>(w.y, o[2], o[3]);
+            codes_to<FMT, T>(w.z, o[4], o[5]);
+            codes_to<FMT, T>(w.w, o[6], o[7]);
+            uint8_t* row = v_s + (p >> 2) * (D * 128) + d * 128;
+            const int j = (p & 3) * 2;
+            *reinterpret_cast<uint4*>(row + ((j ^ (d & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<uint4*>(row + (((j + 1) ^ (d & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+          }
+          tell(v_full + st);
+          if (lane == 0) mbar_arrive(code_empty + cs);
+          ++C;
+        } else {
+          // rows of the pass: K and V alike [128 rows][64 dims] slabs, zeros past the last row
+          const int j0 = (tile - u.cached) * CU_NEW;
+          auto copy = [&](const void* base, long long row_stride, long long head_stride, uint8_t* to) {
+            for (int x = ct; x < 128 * (D / 8); x += CU_CONV * 32) {
+              const int r = x / (D / 8), ch = x % (D / 8);
+              const bool in = j0 + r < u.R;
+              const T* src = static_cast<const T*>(base) + (long long)(u.r0 + (in ? j0 + r : 0)) * row_stride + (long long)u.kvh * head_stride + ch * 8;
+              cp_async16(smem_u32(to) + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4), src, in ? 16 : 0);
+            }
+            cp_async_commit();
+          };
+          if (gt >= 2 && !mbar_wait(k_empty + st, ((gt >> 1) - 1) & 1, status, 312)) { go = false; break; }
+          copy(a.k, a.k_row, a.k_head, k_s);
+          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 313)) { go = false; cp_async_wait<0>(); break; }
+          copy(a.v, a.v_row, a.v_head, v_s);
+          cp_async_wait<1>();
+          if (!q_told) {
+            tell(q_full);
+            q_told = true;
+          }
+          tell(k_full + st);
+          cp_async_wait<0>();
+          // infinities and NaN of V would reach rows that do not see them (0 * NaN): they are taken out here and added at the end, to the rows that do
+          bool found = false;
+          for (int x = ct; x < 128 * (D / 8); x += CU_CONV * 32) {
+            const int r = x / (D / 8), ch = x % (D / 8);
+            uint4* at = reinterpret_cast<uint4*>(v_s + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4));   // (this thread's own copy)
+            uint4 w = *at;
+            if (odd2<T>(w.x) || odd2<T>(w.y) || odd2<T>(w.z) || odd2<T>(w.w)) {
+              found = true;
+              *at = make_uint4(tame2<T>(w.x), tame2<T>(w.y), tame2<T>(w.z), tame2<T>(w.w));
+            }
+          }
+          if (found) odd[U & 7] = 1;
+          tell(v_full + st);
+        }
+      }
+      ++U;
+    } while (go && list.next(u));
+    cp_async_wait<0>();
+  } else {
+    // ---- softmax: a thread a row of the MMA
+    const int grp = warp >> 2, q4 = warp & 3, mrow = q4 * 32 + lane;
+    const int qrow = ROWS == 64 ? mrow & 63 : ROWS == 128 ? mrow : grp * 128 + mrow;
+    const int kh = ROWS == 64 ? mrow >> 6 : 0;
+    constexpr int NK = ROWS == 64 ? 64 : 128, NC = NK / 32;    // keys of a tile that a thread has, in groups of 32
+    const uint32_t lane_base = (uint32_t)(q4 * 32) << 16;
+    const uint32_t s_addr = tmem + lane_base + grp * 128 + kh * 64, p_addr = tmem + lane_base + grp * 128 + kh * 32;
+    const float scale2 = a.scale * 1.44269504088896f;
+    int T0 = 0, C0 = 0, U = 0;
+    bool go = true;
+    do {
+      const int n = u.n, R = u.R, nt = u.tile1 - u.tile, rtile = pl.rt0 + u.rt, rows = min(ROWS, R * G - rtile * ROWS);
+      const int m_all = rtile * ROWS + qrow, qi = m_all / G;
+      const bool live = qi < R;
+      float m_ref = -INFINITY, l_run = 0.f, cv = 1.f;
+      int my_tiles = 0;
+      if (n > 0 && u.tile1 > u.cached) {
+        const int page = c.page(u.s, 0);
+        const float f = page >= 0 ? c.scales[((layer_heads + u.kvh) * c.n_pages + page) * 2 + 1] * code_unit<FMT>() : 0.f;
+        if (f > 0.f) cv = std::is_same<T, bf16>::value ? f : fmaxf(f, 0.0078125f);   // (float16 weights, up to 2^8 / c, stay below 2^15)
+      }
+      const float lgc = __log2f(cv);
+      for (int t = ALT ? (T0 ^ grp) & 1 : 0; t < nt; t += ALT ? 2 : 1, ++my_tiles) {
+        const int gt = T0 + t, tile = u.tile + t;
+        const bool is_new = tile >= u.cached;
+        if (!mbar_wait(s_full + grp, (ALT ? gt >> 1 : gt) & 1, status, 314)) { go = false; break; }
+        __syncwarp();
+        tc_fence_after();
+        uint32_t vis[NC];
+        if (!is_new) {
+#pragma unroll
+          for (int x = 0; x < NC; ++x) {
+            const int left = n - tile * CAM_TILE - kh * 64 - 32 * x;
+            vis[x] = left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1;
+          }
+        } else {
+#pragma unroll
+          for (int x = 0; x < NC / 2; ++x) {
+            const unsigned long long w = live ? sees64(a.mask, a.mask_words, (size_t)(u.r0 + qi), qi, 2 * (tile - u.cached) + kh + x, R) : 0ull;
+            vis[2 * x] = (uint32_t)w;
+            vis[2 * x + 1] = (uint32_t)(w >> 32);
+          }
+        }
+        bool mine = true;
+#pragma unroll
+        for (int x = 0; x < NC; ++x) mine = mine && vis[x] == 0xffffffffu;
+        const bool whole = __all_sync(0xffffffffu, mine);
+        const float4* pg = consts[(C0 + t) & 3] + kh * 4;
+        float top = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < NC; ++x) {
+          uint32_t r[32];
+          tmem_ld32(s_addr + x * 32, r);
+          tmem_ld_wait();
+          if (!whole)
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (!((vis[x] >> j) & 1)) r[j] = 0xff800000u;
+          float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            m0 = fmaxf(m0, __uint_as_float(r[j]));
+            m1 = fmaxf(m1, __uint_as_float(r[16 + j]));
+          }
+          if (is_new) {
+            top = fmaxf(top, fmaf(fmaxf(m0, m1), scale2, lgc));
+          } else {
+            const float4 k0 = pg[2 * x], k1 = pg[2 * x + 1];
+            top = fmaxf(top, fmaxf(fmaf(m0, k0.x, k0.y), fmaf(m1, k1.x, k1.y)));    // (a page of scale 0 without a key to see gives NaN, which the maximum leaves out)
+          }
+        }
+        const bool raise = top > m_ref + CU_RAISE || (m_ref == -INFINITY && top > -INFINITY);
+        const float m_new = raise ? top : m_ref, alpha = raise ? ex2(m_ref - m_new) : 1.f;
+        if (__any_sync(0xffffffffu, raise && my_tiles > 0)) {
+          const uint32_t o_addr = tmem + lane_base + 256u + grp * 128;
+#pragma unroll 1
+          for (int x = 0; x < D / 32; ++x) {
+            uint32_t r[32];
+            tmem_ld32(o_addr + x * 32, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * alpha);
+            tmem_st32(o_addr + x * 32, r);
+          }
+        }
+        m_ref = m_new;
+        l_run *= alpha;
+        const float base = m_ref == -INFINITY ? 0.f : m_ref;
+#pragma unroll
+        for (int x = 0; x < NC; ++x) {
+          uint32_t r[32], pk[16];
+          tmem_ld32(s_addr + x * 32, r);
+          float f[2] = {scale2, scale2}, off[2] = {-base, -base}, inv[2] = {1.f, 1.f};
+          if (!is_new) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float4 k = pg[2 * x + h];
+              f[h] = k.x;
+              off[h] = k.y - base;
+              inv[h] = k.z;
+            }
+          }
+          tmem_ld_wait();
+          float w[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) w[j] = ex2(fmaf(__uint_as_float(r[j]), f[j >> 4], off[j >> 4]));
+          if (!whole)
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (!((vis[x] >> j) & 1)) w[j] = 0.f;
+          float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            s0 += w[j];
+            s1 += w[16 + j];
+          }
+          l_run += s0 * inv[0] + s1 * inv[1];
+          if (is_new) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) pk[j] = pack2<T>(w[2 * j], w[2 * j + 1]);
+          } else {
+            // the order of the places: pair y of a page holds tokens 2 (y / 2) + 8 (y % 2) and the next
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int tok = (j >> 3) * 16 + 2 * ((j & 7) >> 1) + 8 * (j & 1);
+              pk[j] = pack2<T>(w[tok], w[tok + 1]);
+            }
+          }
+          tmem_st16(p_addr + x * 16, pk);             // (over scores that have been read)
+        }
+        if constexpr (ROWS == 64) {
+          uint32_t z[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = 0u;
+          tmem_st32(tmem + lane_base + grp * 128 + (kh ^ 1) * 32, z);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + grp);
+      }
+      // ---- the unit's sums
+      go = go && mbar_wait(o_full, U & 1, status, 315);
+      if (!softmax_and(go)) { go = false; break; }
+      tc_fence_after();
+      const bool whole_unit = u.tile == 0 && u.tile1 == u.tiles, any_odd = odd[U & 7] != 0;
+      float* part = list.part(u, D);
+      // infinities and NaN of V that this row sees
+      auto add_odd = [&](int d, float4& v) {
+        if (!any_odd || !live) return;
+        for (int j = max(0, u.tile - u.cached) * CU_NEW; j < min(R, (u.tile1 - u.cached) * CU_NEW); ++j) {
+          if (!row_sees(a.mask, a.mask_words, u.r0 + qi, qi, j)) continue;
+          const T* vp = static_cast<const T*>(a.v) + (long long)(u.r0 + j) * a.v_row + (long long)u.kvh * a.v_head + d;
+          const float y0 = to_f<T>(vp[0]), y1 = to_f<T>(vp[1]), y2 = to_f<T>(vp[2]), y3 = to_f<T>(vp[3]);
+          if (!(fabsf(y0) < INFINITY)) v.x += y0;
+          if (!(fabsf(y1) < INFINITY)) v.y += y1;
+          if (!(fabsf(y2) < INFINITY)) v.z += y2;
+          if (!(fabsf(y3) < INFINITY)) v.w += y3;
+        }
+      };
+      auto put = [&](int d, float top, float sum, float4 v) {
+        if (qrow >= rows) return;
+        add_odd(d, v);
+        if (whole_unit) {
+          cam_finish<T, D, ROWS>(a, u.r0, rtile, u.kvh, qrow, d, top, sum, v);
+        } else {
+          *reinterpret_cast<float4*>(part + qrow * D + d) = v;
+          if (d == 0) *reinterpret_cast<float2*>(part + ROWS * D + 2 * qrow) = make_float2(top, sum);
+        }
+      };
+      const uint32_t o_addr = tmem + lane_base + 256u;
+      if constexpr (ROWS == 256) {
+#pragma unroll 1
+        for (int x = 0; x < D / 32; ++x) {
+          uint32_t r[32];
+          __syncwarp();
+          tmem_ld32(o_addr + grp * 128 + x * 32, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; j += 4)
+            put(x * 32 + j, m_ref, l_run, make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])));
+        }
+      } else {
+        // both groups' sums of the row lie in its lane: group g takes dims g D / 2 .. of both. The room of q, which has been read, serves for what the threads tell one another
+        float2* ml = reinterpret_cast<float2*>(q_s);
+        ml[grp * 128 + mrow] = make_float2(m_ref, l_run);
+        softmax_bar();
+        const float2 e0 = ml[mrow], e1 = ml[128 + mrow];
+        if constexpr (ROWS == 64) softmax_bar();                // (all have read ml, others' values come over it)
+        const float top = fmaxf(e0.x, e1.x), ref = top == -INFINITY ? 0.f : top, f0 = ex2(e0.x - ref), f1 = ex2(e1.x - ref), sum = f0 * e0.y + f1 * e1.y;
+        const bool has0 = nt > 1 || (T0 & 1) == 0, has1 = nt > 1 || (T0 & 1) == 1;   // (a group without a tile has nothing in its accumulator)
+        float* xb = reinterpret_cast<float*>(q_s);               // [64][D], 16-byte chunk x of row r at x ^ (r % 8)
+        constexpr int DH = D / 2;
+        float4 keep[ROWS == 64 ? DH / 4 : 1];
+#pragma unroll
+        for (int x = 0; x < DH / 32; ++x) {
+          uint32_t r0[32], r1[32];
+          __syncwarp();
+          if (has0) tmem_ld32(o_addr + grp * DH + x * 32, r0);
+          if (has1) tmem_ld32(o_addr + 128 + grp * DH + x * 32, r1);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 32; j += 4) {
+            float4 v;
+            float* y = &v.x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (has0 ? f0 * __uint_as_float(r0[j + e]) : 0.f) + (has1 ? f1 * __uint_as_float(r1[j + e]) : 0.f);
+            if constexpr (ROWS == 128) {
+              put(grp * DH + x * 32 + j, top, sum, v);
+            } else {
+              if (kh == 1) *reinterpret_cast<float4*>(xb + qrow * D + ((((grp * DH + x * 32 + j) >> 2) ^ (qrow & 7)) << 2)) = v;
+              keep[x * 8 + j / 4] = v;
+            }
+          }
+        }
+        if constexpr (ROWS == 64) {
+          // the second half's sums, from the threads of rows 64..
+          if (kh == 1 && grp == 0) xm[qrow] = make_float2(top, sum);
+          softmax_bar();
+          if (kh == 0) {
+            const float2 e = xm[qrow];
+            const float t2 = fmaxf(top, e.x), rf = t2 == -INFINITY ? 0.f : t2, g0 = ex2(top - rf), g1 = ex2(e.x - rf), s2 = g0 * sum + g1 * e.y;
+#pragma unroll
+            for (int x = 0; x < DH / 4; ++x) {
+              const float4 y = *reinterpret_cast<const float4*>(xb + qrow * D + (((grp * DH / 4 + x) ^ (qrow & 7)) << 2));
+              put(grp * DH + 4 * x, t2, s2, make_float4(g0 * keep[x].x + g1 * y.x, g0 * keep[x].y + g1 * y.y, g0 * keep[x].z + g1 * y.z, g0 * keep[x].w + g1 * y.w));
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_empty);
+        tc_fence_before();
+        softmax_bar();                                          // (the accumulators may be written again, ml too)
+      }
+      if (!whole_unit) {
+        const int c0 = list.first_cta(u), c1 = list.last_cta(u);
+        __threadfence();
+        softmax_bar();
+        if (tid == 0) {
+          int* arrive = list.arrive(u);
+          last = atomicAdd(arrive, 1) == c1 - c0;
+          if (last) *arrive = 0;
+        }
+        softmax_bar();
+        if (last) cam_join<T, D, ROWS>(list, u, rows, c0, c1, tid, CU_SOFT * 32);
+        softmax_bar();                                          // (`last` may be written again)
+      }
+      C0 += max(0, min(u.tile1, u.cached) - u.tile);
+      T0 += nt;
+      ++U;
+    } while (go && list.next(u));
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == CU_SOFT + CU_CONV + 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+}  // namespace spec

@@ -37,7 +37,8 @@ def test_bad_caches(lib, kw):
 
 
 @pytest.mark.parametrize("kw", [dict(q=None), dict(out=None), dict(type=3), dict(rows=-1), dict(batch=3), dict(batch=-1), dict(n_heads=6), dict(n_heads=0), dict(layer=2), dict(layer=-1),
-                                dict(max_rows=0), dict(max_rows=1), dict(mask=16, mask_words=0), dict(batch=70000, rows=70000), dict(q=4104), dict(q_row_stride=4), dict(k_head_stride=3), dict(v=8)])
+                                dict(max_rows=0), dict(max_rows=1), dict(mask=16, mask_words=0), dict(batch=70000, rows=70000), dict(q=4104), dict(q_row_stride=4), dict(k_head_stride=3), dict(v=8),
+                                dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))])
 def test_bad_attention(lib, kw):
     ren = {"q_row_stride": "q_row", "k_head_stride": "k_head"}
     v = dict(q=4096, k=4096, v=4096, out=4096, type=1, rows=4, batch=2, n_heads=8, layer=0, max_rows=2, q_row=512, q_head=64, k_row=256, k_head=64, v_row=256, v_head=64, scale=0.1)
