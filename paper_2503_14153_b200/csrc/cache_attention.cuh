@@ -404,29 +404,47 @@ __device__ __forceinline__ void cam_finish(const CacheAttnArgs& a, int r0, int r
   if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.693147180559945f;
 }
 
-// The parts of a unit, all left by now, added in the order of their CTAs by `threads` threads.
-template <typename T, int D, int MT, typename L>
-__device__ __forceinline__ void cam_join(const L& list, const CamCursor& u, int rows, int c0, int c1, int tid, int threads) {
+// The parts of a unit, all left by now, added in the order of their CTAs by THREADS threads, each with four rows in flight (one at a time, 64 rows of five parts took 13 us).
+template <typename T, int D, int MT, int THREADS, typename L>
+__device__ __forceinline__ void cam_join(const L& list, const CamCursor& u, int rows, int c0, int c1, int tid) {
   __threadfence();
-  for (int x = tid; x < rows * (D / 4); x += threads) {
-    const int r = x / (D / 4), d = x % (D / 4) * 4;
-    float top = -INFINITY, sum = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+  constexpr int RP = THREADS / (D / 4), RB = 4;   // rows side by side; rows a thread
+  const int d = tid % (D / 4) * 4;
+  for (int r0 = tid / (D / 4); r0 < rows; r0 += RP * RB) {
+    float top[RB], sum[RB];
+    float4 v[RB];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+      top[j] = -INFINITY;
+      sum[j] = 0.f;
+      v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll 2
     for (int k = c0; k <= c1; ++k) {
       const float* in = list.part_of(k, c0, D);
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(in + MT * D + 2 * r));
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(in + r * D + d));
-      const float now = fmaxf(top, ml.x), ref = now == -INFINITY ? 0.f : now;
-      const float f = ex2(top - ref), h = ex2(ml.x - ref);
-      sum = f * sum + h * ml.y;
-      v.x = f * v.x + h * y.x;
-      v.y = f * v.y + h * y.y;
-      v.z = f * v.z + h * y.z;
-      v.w = f * v.w + h * y.w;
-      top = now;
+      float2 e[RB];
+      float4 y[RB];
+#pragma unroll
+      for (int j = 0; j < RB; ++j) {
+        const int r = min(r0 + j * RP, rows - 1);
+        e[j] = __ldcg(reinterpret_cast<const float2*>(in + MT * D + 2 * r));
+        y[j] = __ldcg(reinterpret_cast<const float4*>(in + r * D + d));
+      }
+#pragma unroll
+      for (int j = 0; j < RB; ++j) {
+        const float now = fmaxf(top[j], e[j].x), ref = now == -INFINITY ? 0.f : now;
+        const float f = ex2(top[j] - ref), h = ex2(e[j].x - ref);
+        sum[j] = f * sum[j] + h * e[j].y;
+        v[j].x = f * v[j].x + h * y[j].x;
+        v[j].y = f * v[j].y + h * y[j].y;
+        v[j].z = f * v[j].z + h * y[j].z;
+        v[j].w = f * v[j].w + h * y[j].w;
+        top[j] = now;
+      }
     }
-    cam_finish<T, D, MT>(list.a, u.r0, list.pl.rt0 + u.rt, u.kvh, r, d, top, sum, v);
+#pragma unroll
+    for (int j = 0; j < RB; ++j)
+      if (r0 + j * RP < rows) cam_finish<T, D, MT>(list.a, u.r0, list.pl.rt0 + u.rt, u.kvh, r0 + j * RP, d, top[j], sum[j], v[j]);
   }
 }
 
@@ -827,7 +845,7 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
         if (last) *arrive = 0;
       }
       __syncthreads();
-      if (last) cam_join<T, D, MT>(list, use, rows, c0, c1, tid, CAM_THREADS);
+      if (last) cam_join<T, D, MT, CAM_THREADS>(list, use, rows, c0, c1, tid);
     }
   }
   cp_async_wait<0>();

@@ -15,15 +15,15 @@
 
 namespace spec {
 
-constexpr int CU_SOFT = 8, CU_CONV = 4;                       // softmax and converter warps
+constexpr int CU_SOFT = 8, CU_CONV = 6;                       // softmax and converter warps
 constexpr int CU_WARPS = CU_SOFT + CU_CONV + 2, CU_THREADS = 32 * CU_WARPS;
 constexpr int CU_PAIRS = 160;                                 // (sequence, row tile) pairs a launch can deal
 constexpr int CU_NEW = 128;                                   // rows of the pass a tile
 constexpr float CU_RAISE = 8.f;
 
-__host__ __device__ constexpr int cu_code_stages(int ROWS) { return ROWS == 256 ? 1 : 2; }
+__host__ __device__ constexpr int cu_code_stages(int ROWS) { return ROWS == 256 ? 2 : 3; }
 __host__ __device__ constexpr size_t cu_smem(int D, int ROWS) {
-  return 1024 + (size_t)(ROWS == 256 ? 2 : 1) * 128 * D * 2 /*Q*/ + 2 * (size_t)(2 * 128 * D * 2) /*K, V*/ + (size_t)cu_code_stages(ROWS) * 256 * D /*codes*/;
+  return 1024 + (size_t)(ROWS == 256 ? 2 : 1) * 128 * D * 2 /*Q*/ + 3 * (size_t)(128 * D * 2) /*K, two of V*/ + (size_t)cu_code_stages(ROWS) * 256 * D /*codes*/;
 }
 
 // D[tmem] (+)= A[tmem] * B[smem]
@@ -49,16 +49,17 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   constexpr int NQ = ROWS == 256 ? 2 : 1;
   constexpr bool ALT = ROWS != 256;                            // the groups take alternate tiles
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(16) uint64_t bars[22];
-  __shared__ float4 consts[4][CAM_PAGES];                      // a page's scale of K, log2 and reciprocal of its scale of V; by cached tile
+  __shared__ __align__(16) uint64_t bars[20];
+  __shared__ float2 consts[8][CAM_PAGES];                      // a page's scale of K with the score's factors, log2 of its scale of V; by cached tile
   __shared__ float2 xm[64];
   __shared__ int pre[CU_PAIRS + 1], scan[CU_WARPS], odd[8], last;
   __shared__ uint32_t tmem_slot;
   const uint32_t raw = smem_u32(smem_raw);
   uint8_t* q_s = smem_raw + (((raw + 1023u) & ~1023u) - raw);
-  uint8_t* kv_s = q_s + NQ * OPER;                             // [2 stages][K, V]
-  uint8_t* code_s = kv_s + 4 * OPER;
-  uint64_t *code_full = bars, *code_empty = bars + 2, *k_full = bars + 4, *k_empty = bars + 6, *v_full = bars + 8, *v_empty = bars + 10, *s_full = bars + 12, *p_full = bars + 14, *q_full = bars + 16,
+  uint8_t* k_s = q_s + NQ * OPER;
+  uint8_t* v_s0 = k_s + OPER;                                  // [2]
+  uint8_t* code_s = v_s0 + 2 * OPER;                           // [CS]
+  uint64_t *code_full = bars, *code_empty = bars + 3, *k_full = bars + 6, *k_empty = bars + 7, *v_full = bars + 8, *v_empty = bars + 10, *s_full = bars + 12, *p_full = bars + 14, *q_full = bars + 16,
            *q_empty = bars + 17, *o_full = bars + 18;
   const CacheView& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.H / c.kv;
@@ -69,11 +70,13 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   CamCursor u;
   if (!list.first(u)) return;
   if (tid == 0) {
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < CS; ++i) {
       mbar_init(code_full + i, 1);
       mbar_init(code_empty + i, CU_CONV);
-      mbar_init(k_full + i, CU_CONV);
-      mbar_init(k_empty + i, 1);
+    }
+    mbar_init(k_full, CU_CONV);
+    mbar_init(k_empty, 1);
+    for (int i = 0; i < 2; ++i) {
       mbar_init(v_full + i, CU_CONV);
       mbar_init(v_empty + i, 1);
       mbar_init(s_full + i, 1);
@@ -81,7 +84,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
     }
     for (int i = 0; i < 8; ++i) odd[i] = 0;
     mbar_init(q_full, CU_CONV);
-    mbar_init(q_empty, ALT ? 1 + CU_SOFT : 1);
+    mbar_init(q_empty, 1 + CU_SOFT);
     mbar_init(o_full, 1);
     mbar_fence_init();
   }
@@ -115,7 +118,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
         if (C >= CS) go = mbar_wait(code_empty + cs, ((C / CS) - 1) & 1, status, 301);
         if (!__all_sync(0xffffffffu, go)) { go = false; break; }
         const float v = sc.y > 0.f ? sc.y * code_unit<FMT>() : 9.094947017729282e-13f;    // (a block of zeros: 2^-40 does not raise the reference)
-        if (lane < CAM_PAGES) consts[C & 3][lane] = make_float4(sc.x * code_unit<FMT>() * a.scale * 1.44269504088896f, __log2f(v), __fdividef(1.f, v), 0.f);
+        if (lane < CAM_PAGES) consts[C & 7][lane] = make_float2(sc.x * code_unit<FMT>() * a.scale * 1.44269504088896f, __log2f(v));
         const uint32_t valid = __ballot_sync(0xffffffffu, page >= 0);
         if (lane == 0) mbar_expect_tx(code_full + cs, __popc(valid) * 2 * BLOCK);
         __syncwarp();
@@ -139,17 +142,16 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       do {
         const int nt = u.tile1 - u.tile;
         auto mma_s = [&](int t, int x) {           // scores of tile t; x: S buffer and, with 256 rows, Q tile
-          const int st = (T0 + t) & 1;
           if (t == 0 && x == (ALT ? (T0 & 1) : 0) && !mbar_wait(q_full, U & 1, status, 303)) return false;
-          if (!mbar_wait(k_full + st, ((T0 + t) >> 1) & 1, status, 304)) return false;
+          if (!mbar_wait(k_full, (T0 + t) & 1, status, 304)) return false;
           tc_fence_after();
-          const uint32_t k_addr = smem_u32(kv_s + st * 2 * OPER), qa = q_addr + (ALT ? 0 : x * OPER);
+          const uint32_t k_addr = smem_u32(k_s), qa = q_addr + (ALT ? 0 : x * OPER);
 #pragma unroll
           for (int j = 0; j < D / 16; ++j)
             tc_mma_f16(tmem + x * 128, make_kmajor_sw128_desc(qa + (j >> 2) * 16384) + 2 * (j & 3), make_kmajor_sw128_desc(k_addr + (j >> 2) * 16384) + 2 * (j & 3), idesc_s, j > 0);
           tc_commit(s_full + x);
           if (ALT || x == 1) {
-            tc_commit(k_empty + st);
+            tc_commit(k_empty);
             if (t == nt - 1) tc_commit(q_empty);
           }
           return true;
@@ -158,7 +160,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           const int gt = T0 + t, st = gt & 1;
           if (!mbar_wait(p_full + x, (ALT ? gt >> 1 : gt) & 1, status, 305) || !mbar_wait(v_full + st, (gt >> 1) & 1, status, 306)) return false;
           tc_fence_after();
-          const uint32_t v_addr = smem_u32(kv_s + st * 2 * OPER + OPER);
+          const uint32_t v_addr = smem_u32(v_s0 + st * OPER);
           const bool is_new = u.tile + t >= u.cached;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {             // 16 keys
@@ -194,66 +196,58 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
+    constexpr int CT = CU_CONV * 32, CHUNKS = CAM_PAGES * D;   // 16-byte chunks of a tile's K, or V
+    auto widen = [&](const uint4& w, uint8_t* row, int j, int x) {     // 16 codes to 16-byte chunks j and j + 1 of a 128-byte row, swizzled by x
+      uint32_t o[8];
+      codes_to<FMT, T>(w.x, o[0], o[1]);
+      codes_to<FMT, T>(w.y, o[2], o[3]);
+      codes_to<FMT, T>(w.z, o[4], o[5]);
+      codes_to<FMT, T>(w.w, o[6], o[7]);
+      *reinterpret_cast<uint4*>(row + ((j ^ x) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<uint4*>(row + (((j + 1) ^ x) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+    };
     int gt = 0, C = 0, U = 0;
     bool go = true;
     do {
       const int rtile = pl.rt0 + u.rt;
-      // q: row r of the tile at row r (64 rows: and at r + 64), 16-byte chunk ch at chunk ch ^ (r % 8) of its 128 bytes
-      if (U > 0) go = mbar_wait(q_empty, (U - 1) & 1, status, 308);
-      if (!go) break;
-      for (int x = ct; x < NQ * 128 * (D / 8); x += CU_CONV * 32) {
-        const int r = x / (D / 8), ch = x % (D / 8), m = rtile * ROWS + (ROWS == 64 ? r & 63 : r), i = m / G;
-        const bool live = i < u.R;
-        const T* src = static_cast<const T*>(a.q) + (long long)(u.r0 + (live ? i : 0)) * a.q_row + (long long)(u.kvh * G + (live ? m - i * G : 0)) * a.q_head + ch * 8;
-        cp_async16(smem_u32(q_s) + (r >> 7) * OPER + (ch >> 3) * 16384 + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4), src, live ? 16 : 0);
-      }
-      cp_async_commit();
+      // q: row r of the tile at row r (64 rows: and at r + 64), 16-byte chunk ch at chunk ch ^ (r % 8) of its 128 bytes. Its room is free when the last unit's output is through.
+      auto ask_q = [&]() {
+        if (U > 0 && !mbar_wait(q_empty, (U - 1) & 1, status, 308)) return false;
+        for (int x = ct; x < NQ * 128 * (D / 8); x += CT) {
+          const int r = x / (D / 8), ch = x % (D / 8), m = rtile * ROWS + (ROWS == 64 ? r & 63 : r), i = m / G;
+          const bool live = i < u.R;
+          const T* src = static_cast<const T*>(a.q) + (long long)(u.r0 + (live ? i : 0)) * a.q_row + (long long)(u.kvh * G + (live ? m - i * G : 0)) * a.q_head + ch * 8;
+          cp_async16(smem_u32(q_s) + (r >> 7) * OPER + (ch >> 3) * 16384 + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4), src, live ? 16 : 0);
+        }
+        cp_async_commit();
+        return true;
+      };
       if (ct == 0) odd[(U + 4) & 7] = 0;    // (no unit that is still worked on: the roles are at most three apart)
-      bool q_told = false;
       for (int tile = u.tile; tile < u.tile1; ++tile, ++gt) {
         const int st = gt & 1;
-        uint8_t* k_s = kv_s + st * 2 * OPER;
-        uint8_t* v_s = k_s + OPER;
+        const bool first = tile == u.tile;
+        uint8_t* v_s = v_s0 + st * OPER;
         if (tile < u.cached) {
           const int cs = C % CS;
-          go = mbar_wait(code_full + cs, (C / CS) & 1, status, 309) && (gt < 2 || mbar_wait(k_empty + st, ((gt >> 1) - 1) & 1, status, 310));
+          go = mbar_wait(code_full + cs, (C / CS) & 1, status, 309) && (gt < 1 || mbar_wait(k_empty, (gt - 1) & 1, status, 310));
           if (!go) break;
           const uint4* codes = reinterpret_cast<const uint4*>(code_s + (size_t)cs * 256 * D);
-#pragma unroll 4
-          for (int it = 0; it < CAM_PAGES * D / (CU_CONV * 32); ++it) {
-            const int x = it * CU_CONV * 32 + ct, p = x / D, y = x % D;
-            const uint4 w = codes[p * (2 * D) + y];
-            const int ch = (y >> 3) % (D / 16), key = p * 16 + (y / (D / 2)) * 8 + (y & 7);
-            uint32_t o[8];
-            codes_to<FMT, T>(w.x, o[0], o[1]);
-            codes_to<FMT, T>(w.y, o[2], o[3]);
-            codes_to<FMT, T>(w.z, o[4], o[5]);
-            codes_to<FMT, T>(w.w, o[6], o[7]);
-            uint8_t* row = k_s + (ch >> 2) * 16384 + key * 128;
-            const int j = (ch & 3) * 2;
-            *reinterpret_cast<uint4*>(row + ((j ^ (key & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<uint4*>(row + (((j + 1) ^ (key & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll 3
+          for (int x = ct; x < CHUNKS; x += CT) {
+            const int p = x / D, y = x % D, ch = (y >> 3) % (D / 16), key = p * 16 + (y / (D / 2)) * 8 + (y & 7);
+            widen(codes[p * (2 * D) + y], k_s + (ch >> 2) * 16384 + key * 128, (ch & 3) * 2, key & 7);
           }
-          if (!q_told) {
+          tell(k_full);
+          if (first && !ask_q()) { go = false; break; }
+          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 311)) { go = false; break; }
+#pragma unroll 3
+          for (int x = ct; x < CHUNKS; x += CT) {
+            const int p = x / D, d = x % D;
+            widen(codes[p * (2 * D) + D + d], v_s + (p >> 2) * (D * 128) + d * 128, (p & 3) * 2, d & 7);
+          }
+          if (first) {
             cp_async_wait<0>();
             tell(q_full);
-            q_told = true;
-          }
-          tell(k_full + st);
-          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 311)) { go = false; break; }
-#pragma unroll 4
-          for (int it = 0; it < CAM_PAGES * D / (CU_CONV * 32); ++it) {
-            const int x = it * CU_CONV * 32 + ct, p = x / D, d = x % D;
-            const uint4 w = codes[p * (2 * D) + D + d];
-            uint32_t o[8];
-            codes_to<FMT, T>(w.x, o[0], o[1]);
-            codes_to<FMT, T>(w.y, o[2], o[3]);
-            codes_to<FMT, T>(w.z, o[4], o[5]);
-            codes_to<FMT, T>(w.w, o[6], o[7]);
-            uint8_t* row = v_s + (p >> 2) * (D * 128) + d * 128;
-            const int j = (p & 3) * 2;
-            *reinterpret_cast<uint4*>(row + ((j ^ (d & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<uint4*>(row + (((j + 1) ^ (d & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
           }
           tell(v_full + st);
           if (lane == 0) mbar_arrive(code_empty + cs);
@@ -262,7 +256,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           // rows of the pass: K and V alike [128 rows][64 dims] slabs, zeros past the last row
           const int j0 = (tile - u.cached) * CU_NEW;
           auto copy = [&](const void* base, long long row_stride, long long head_stride, uint8_t* to) {
-            for (int x = ct; x < 128 * (D / 8); x += CU_CONV * 32) {
+            for (int x = ct; x < 128 * (D / 8); x += CT) {
               const int r = x / (D / 8), ch = x % (D / 8);
               const bool in = j0 + r < u.R;
               const T* src = static_cast<const T*>(base) + (long long)(u.r0 + (in ? j0 + r : 0)) * row_stride + (long long)u.kvh * head_stride + ch * 8;
@@ -270,20 +264,18 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
             }
             cp_async_commit();
           };
-          if (gt >= 2 && !mbar_wait(k_empty + st, ((gt >> 1) - 1) & 1, status, 312)) { go = false; break; }
+          if (gt >= 1 && !mbar_wait(k_empty, (gt - 1) & 1, status, 312)) { go = false; break; }
           copy(a.k, a.k_row, a.k_head, k_s);
-          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 313)) { go = false; cp_async_wait<0>(); break; }
+          if (first && !ask_q()) { go = false; break; }
+          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 313)) { go = false; break; }
           copy(a.v, a.v_row, a.v_head, v_s);
           cp_async_wait<1>();
-          if (!q_told) {
-            tell(q_full);
-            q_told = true;
-          }
-          tell(k_full + st);
+          tell(k_full);
+          if (first) tell(q_full);
           cp_async_wait<0>();
           // infinities and NaN of V would reach rows that do not see them (0 * NaN): they are taken out here and added at the end, to the rows that do
           bool found = false;
-          for (int x = ct; x < 128 * (D / 8); x += CU_CONV * 32) {
+          for (int x = ct; x < 128 * (D / 8); x += CT) {
             const int r = x / (D / 8), ch = x % (D / 8);
             uint4* at = reinterpret_cast<uint4*>(v_s + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4));   // (this thread's own copy)
             uint4 w = *at;
@@ -347,7 +339,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
 #pragma unroll
         for (int x = 0; x < NC; ++x) mine = mine && vis[x] == 0xffffffffu;
         const bool whole = __all_sync(0xffffffffu, mine);
-        const float4* pg = consts[(C0 + t) & 3] + kh * 4;
+        const float2* pg = consts[(C0 + t) & 7] + kh * 4;
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < NC; ++x) {
@@ -367,7 +359,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           if (is_new) {
             top = fmaxf(top, fmaf(fmaxf(m0, m1), scale2, lgc));
           } else {
-            const float4 k0 = pg[2 * x], k1 = pg[2 * x + 1];
+            const float2 k0 = pg[2 * x], k1 = pg[2 * x + 1];
             top = fmaxf(top, fmaxf(fmaf(m0, k0.x, k0.y), fmaf(m1, k1.x, k1.y)));    // (a page of scale 0 without a key to see gives NaN, which the maximum leaves out)
           }
         }
@@ -396,10 +388,10 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           if (!is_new) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float4 k = pg[2 * x + h];
+              const float2 k = pg[2 * x + h];
               f[h] = k.x;
               off[h] = k.y - base;
-              inv[h] = k.z;
+              inv[h] = ex2(-k.y);
             }
           }
           tmem_ld_wait();
@@ -447,9 +439,8 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       tc_fence_after();
       const bool whole_unit = u.tile == 0 && u.tile1 == u.tiles, any_odd = odd[U & 7] != 0;
       float* part = list.part(u, D);
-      // infinities and NaN of V that this row sees
+      // infinities and NaN of V that this row sees, dims d .. d + 3
       auto add_odd = [&](int d, float4& v) {
-        if (!any_odd || !live) return;
         for (int j = max(0, u.tile - u.cached) * CU_NEW; j < min(R, (u.tile1 - u.cached) * CU_NEW); ++j) {
           if (!row_sees(a.mask, a.mask_words, u.r0 + qi, qi, j)) continue;
           const T* vp = static_cast<const T*>(a.v) + (long long)(u.r0 + j) * a.v_row + (long long)u.kvh * a.v_head + d;
@@ -460,80 +451,132 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           if (!(fabsf(y3) < INFINITY)) v.w += y3;
         }
       };
-      auto put = [&](int d, float top, float sum, float4 v) {
-        if (qrow >= rows) return;
-        add_odd(d, v);
+      // The row's (max, sum) and what its values are multiplied by before they leave: a whole unit's rows are finished here, a part's stay as they are.
+      auto head = [&](float top, float sum) {
+        if (live && qrow < rows) {
+          if (!whole_unit) *reinterpret_cast<float2*>(part + ROWS * D + 2 * qrow) = make_float2(top, sum);
+          else if (a.lse) a.lse[(size_t)(u.r0 + qi) * a.H + u.kvh * G + m_all - qi * G] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.693147180559945f;
+        }
+        return !whole_unit ? 1.f : sum > 0.f || sum != sum ? 1.f / sum : 0.f;   // (a sum that is NaN makes the row NaN)
+      };
+      // four values of row r of the tile on their way out
+      auto put = [&](int r, int d, float4 v) {
+        if (r >= rows) return;
         if (whole_unit) {
-          cam_finish<T, D, ROWS>(a, u.r0, rtile, u.kvh, qrow, d, top, sum, v);
+          const int mm = rtile * ROWS + r, i = mm / G;
+          *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + ((size_t)(u.r0 + i) * a.H + u.kvh * G + mm - i * G) * D + d) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
         } else {
-          *reinterpret_cast<float4*>(part + qrow * D + d) = v;
-          if (d == 0) *reinterpret_cast<float2*>(part + ROWS * D + 2 * qrow) = make_float2(top, sum);
+          *reinterpret_cast<float4*>(part + r * D + d) = v;
         }
       };
+      // The room of q, which has been read, serves for what the threads tell one another and for turning rows: a thread has a row, a warp writes out whole rows.
       const uint32_t o_addr = tmem + lane_base + 256u;
-      if constexpr (ROWS == 256) {
-#pragma unroll 1
-        for (int x = 0; x < D / 32; ++x) {
-          uint32_t r[32];
-          __syncwarp();
-          tmem_ld32(o_addr + grp * 128 + x * 32, r);
-          tmem_ld_wait();
-#pragma unroll
-          for (int j = 0; j < 32; j += 4)
-            put(x * 32 + j, m_ref, l_run, make_float4(__uint_as_float(r[j]), __uint_as_float(r[j + 1]), __uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])));
-        }
-      } else {
-        // both groups' sums of the row lie in its lane: group g takes dims g D / 2 .. of both. The room of q, which has been read, serves for what the threads tell one another
+      float f0 = 1.f, f1 = 0.f, top = m_ref, sum = l_run;
+      bool has0 = true, has1 = false;
+      if constexpr (ALT) {
+        // both groups' sums of the row lie in its lane
         float2* ml = reinterpret_cast<float2*>(q_s);
         ml[grp * 128 + mrow] = make_float2(m_ref, l_run);
         softmax_bar();
         const float2 e0 = ml[mrow], e1 = ml[128 + mrow];
-        if constexpr (ROWS == 64) softmax_bar();                // (all have read ml, others' values come over it)
-        const float top = fmaxf(e0.x, e1.x), ref = top == -INFINITY ? 0.f : top, f0 = ex2(e0.x - ref), f1 = ex2(e1.x - ref), sum = f0 * e0.y + f1 * e1.y;
-        const bool has0 = nt > 1 || (T0 & 1) == 0, has1 = nt > 1 || (T0 & 1) == 1;   // (a group without a tile has nothing in its accumulator)
-        float* xb = reinterpret_cast<float*>(q_s);               // [64][D], 16-byte chunk x of row r at x ^ (r % 8)
-        constexpr int DH = D / 2;
-        float4 keep[ROWS == 64 ? DH / 4 : 1];
+        softmax_bar();                                          // (all have read: values come over it)
+        top = fmaxf(e0.x, e1.x);
+        const float ref = top == -INFINITY ? 0.f : top;
+        f0 = ex2(e0.x - ref);
+        f1 = ex2(e1.x - ref);
+        sum = f0 * e0.y + f1 * e1.y;
+        has0 = nt > 1 || (T0 & 1) == 0;                         // (a group without a tile has nothing in its accumulator)
+        has1 = nt > 1 || (T0 & 1) == 1;
+      }
+      // 32 of the row's values, both groups' together
+      auto load = [&](int col, float (&v)[32]) {
+        __syncwarp();
+        if constexpr (ALT) {
 #pragma unroll
-        for (int x = 0; x < DH / 32; ++x) {
-          uint32_t r0[32], r1[32];
-          __syncwarp();
-          if (has0) tmem_ld32(o_addr + grp * DH + x * 32, r0);
-          if (has1) tmem_ld32(o_addr + 128 + grp * DH + x * 32, r1);
+          for (int h = 0; h < 32; h += 16) {
+            uint32_t r0[16], r1[16];
+            tmem_ld16(o_addr + col + h, r0);
+            tmem_ld16(o_addr + 128 + col + h, r1);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[h + j] = (has0 ? f0 * __uint_as_float(r0[j]) : 0.f) + (has1 ? f1 * __uint_as_float(r1[j]) : 0.f);
+          }
+        } else {
+          uint32_t r0[32];
+          tmem_ld32(o_addr + grp * 128 + col, r0);
           tmem_ld_wait();
 #pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r0[j]);
+        }
+      };
+      if constexpr (ROWS == 64) {
+        // a group has half of the dims; the second half's sums go over to the threads of the first: [64][D], 16-byte chunk x of row r at x ^ (r % 8)
+        float* xb = reinterpret_cast<float*>(q_s) + qrow * D;
+        constexpr int DH = D / 2;
+        if (kh == 1) {
+          if (grp == 0) xm[qrow] = make_float2(top, sum);
+#pragma unroll 1
+          for (int x = 0; x < DH; x += 32) {
+            float v[32];
+            load(grp * DH + x, v);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(xb + ((((grp * DH + x + j) >> 2) ^ (qrow & 7)) << 2)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          }
+        }
+        softmax_bar();
+        if (kh == 0) {
+          const float2 e = xm[qrow];
+          const float t2 = fmaxf(top, e.x), rf = t2 == -INFINITY ? 0.f : t2, s2 = ex2(top - rf) * sum + ex2(e.x - rf) * e.y;
+          const float k = grp == 0 ? head(t2, s2) : !whole_unit ? 1.f : s2 > 0.f || s2 != s2 ? 1.f / s2 : 0.f, g0 = k * ex2(top - rf), g1 = k * ex2(e.x - rf);
+#pragma unroll 1
+          for (int x = 0; x < DH; x += 32) {
+            float v[32];
+            load(grp * DH + x, v);
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              float4* at = reinterpret_cast<float4*>(xb + ((((grp * DH + x + j) >> 2) ^ (qrow & 7)) << 2));
+              const float4 y = *at;
+              float4 w = make_float4(g0 * v[j] + g1 * y.x, g0 * v[j + 1] + g1 * y.y, g0 * v[j + 2] + g1 * y.z, g0 * v[j + 3] + g1 * y.w);
+              if (any_odd && live) add_odd(grp * DH + x + j, w);
+              *at = w;
+            }
+          }
+        }
+        softmax_bar();
+        const float4* all = reinterpret_cast<const float4*>(q_s);
+        for (int x = tid; x < rows * (D / 4); x += CU_SOFT * 32) {
+          const int r = x / (D / 4), d4 = x % (D / 4);
+          put(r, d4 * 4, all[r * (D / 4) + (d4 ^ (r & 7))]);
+        }
+      } else {
+        // 32 dims at a time through [128 rows][32]: with 128 rows a group has half of the dims, with 256 all of its rows'
+        const float k = ROWS == 256 || grp == 0 ? head(top, sum) : !whole_unit ? 1.f : sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+        float* xb = reinterpret_cast<float*>(q_s) + grp * 4096;
+        auto group_bar = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(3 + grp) : "memory"); };
+        constexpr int DG = ROWS == 128 ? D / 2 : D;
+        const int d0 = ROWS == 128 ? grp * DG : 0;
+#pragma unroll 1
+        for (int x = 0; x < DG; x += 32) {
+          float v[32];
+          load(d0 + x, v);
+#pragma unroll
           for (int j = 0; j < 32; j += 4) {
-            float4 v;
-            float* y = &v.x;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (has0 ? f0 * __uint_as_float(r0[j + e]) : 0.f) + (has1 ? f1 * __uint_as_float(r1[j + e]) : 0.f);
-            if constexpr (ROWS == 128) {
-              put(grp * DH + x * 32 + j, top, sum, v);
-            } else {
-              if (kh == 1) *reinterpret_cast<float4*>(xb + qrow * D + ((((grp * DH + x * 32 + j) >> 2) ^ (qrow & 7)) << 2)) = v;
-              keep[x * 8 + j / 4] = v;
-            }
+            float4 w = make_float4(k * v[j], k * v[j + 1], k * v[j + 2], k * v[j + 3]);
+            if (any_odd && live) add_odd(d0 + x + j, w);
+            *reinterpret_cast<float4*>(xb + mrow * 32 + (((j >> 2) ^ (mrow & 7)) << 2)) = w;
           }
-        }
-        if constexpr (ROWS == 64) {
-          // the second half's sums, from the threads of rows 64..
-          if (kh == 1 && grp == 0) xm[qrow] = make_float2(top, sum);
-          softmax_bar();
-          if (kh == 0) {
-            const float2 e = xm[qrow];
-            const float t2 = fmaxf(top, e.x), rf = t2 == -INFINITY ? 0.f : t2, g0 = ex2(top - rf), g1 = ex2(e.x - rf), s2 = g0 * sum + g1 * e.y;
-#pragma unroll
-            for (int x = 0; x < DH / 4; ++x) {
-              const float4 y = *reinterpret_cast<const float4*>(xb + qrow * D + (((grp * DH / 4 + x) ^ (qrow & 7)) << 2));
-              put(grp * DH + 4 * x, t2, s2, make_float4(g0 * keep[x].x + g1 * y.x, g0 * keep[x].y + g1 * y.y, g0 * keep[x].z + g1 * y.z, g0 * keep[x].w + g1 * y.w));
-            }
+          group_bar();
+          for (int y = tid & 127; y < 128 * 8; y += 128) {
+            const int r = y >> 3, c4 = y & 7;
+            put((ROWS == 256 ? grp * 128 : 0) + r, d0 + x + c4 * 4, *reinterpret_cast<const float4*>(xb + r * 32 + ((c4 ^ (r & 7)) << 2)));
           }
+          group_bar();
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_empty);
-        tc_fence_before();
-        softmax_bar();                                          // (the accumulators may be written again, ml too)
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty);
+      tc_fence_before();
+      if constexpr (ALT) softmax_bar();                         // (the accumulators may be written again)
       if (!whole_unit) {
         const int c0 = list.first_cta(u), c1 = list.last_cta(u);
         __threadfence();
@@ -544,7 +587,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           if (last) *arrive = 0;
         }
         softmax_bar();
-        if (last) cam_join<T, D, ROWS>(list, u, rows, c0, c1, tid, CU_SOFT * 32);
+        if (last) cam_join<T, D, ROWS, CU_SOFT * 32>(list, u, rows, c0, c1, tid);
         softmax_bar();                                          // (`last` may be written again)
       }
       C0 += max(0, min(u.tile1, u.cached) - u.tile);
