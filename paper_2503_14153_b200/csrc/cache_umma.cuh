@@ -9,17 +9,20 @@
 //   8 softmax warps   in two groups, a thread a row: S out of tensor memory, weights back into the same columns as the A operand of P V.
 // With 64 rows the rows are given twice to the 128-row MMA, rows 64.. taking care of the second half of every tile's keys (P is block-diagonal), so that all four
 // SM quarters work; with 64 and 128 the groups take alternate tiles, each with its own S and O; with 256 each group has 128 rows and takes all tiles, so that a tile is converted once for 256 rows.
-// The running reference is raised only when a tile's maximum exceeds it by more than 2^8; a group's O row is then rescaled in place.
+// There is no pass for the maximum: weights are taken against the running reference as it is, and only where 16 keys together weigh more than cu_raise is it raised to the largest of them, O
+// and the tile's weights so far being rescaled in place; after a row's first keys that almost never happens.
 #pragma once
 #include "cache_attention.cuh"
 
 namespace spec {
 
-constexpr int CU_SOFT = 8, CU_CONV = 6;                       // softmax and converter warps
+constexpr int CU_SOFT = 8, CU_CONV = 4;                       // softmax and converter warps
 constexpr int CU_WARPS = CU_SOFT + CU_CONV + 2, CU_THREADS = 32 * CU_WARPS;
-constexpr int CU_PAIRS = 160;                                 // (sequence, row tile) pairs a launch can deal
+constexpr int CU_PAIRS = 256;                                 // (sequence, row tile) pairs a launch can deal
 constexpr int CU_NEW = 128;                                   // rows of the pass a tile
-constexpr float CU_RAISE = 8.f;
+// What 16 keys may weigh together before the reference is raised. bf16 weights and float32 sums lose nothing at any size (raising at 128: 313 us for a prompt that takes 250); float16 weights, up to
+// 2^7 times this with the rows of the pass, stay below 2^15.
+template <typename T> __host__ __device__ constexpr float cu_raise() { return std::is_same<T, bf16>::value ? 1.1529215046068470e18f : 256.f; }
 
 __host__ __device__ constexpr int cu_code_stages(int ROWS) { return ROWS == 256 ? 2 : 3; }
 __host__ __device__ constexpr size_t cu_smem(int D, int ROWS) {
@@ -43,6 +46,28 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 
+// pairs of floats in one register pair: one instruction for two
+__device__ __forceinline__ unsigned long long pair2(float lo, float hi) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpair2(unsigned long long v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return unpair2(r);
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 template <typename T, int D, int FMT, int ROWS>
 __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnArgs a, CamPlan pl) {
   constexpr int CS = cu_code_stages(ROWS), BLOCK = CACHE_PAGE * D, OPER = 128 * D * 2;   // OPER: bytes of one operand tile (Q, K or V)
@@ -51,7 +76,6 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(16) uint64_t bars[20];
   __shared__ float2 consts[8][CAM_PAGES];                      // a page's scale of K with the score's factors, log2 of its scale of V; by cached tile
-  __shared__ float2 xm[64];
   __shared__ int pre[CU_PAIRS + 1], scan[CU_WARPS], odd[8], last;
   __shared__ uint32_t tmem_slot;
   const uint32_t raw = smem_u32(smem_raw);
@@ -99,34 +123,50 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   const size_t layer_heads = (size_t)a.layer * c.kv;
 
   if (warp == CU_SOFT + CU_CONV) {
-    // ---- producer: the pages of cached tiles. Lane p < 8 has page p of a tile; its number and scales are asked for a tile ahead.
+    // ---- producer: the pages of cached tiles, four tiles a batch: lane l has page l % 8 of the batch's tile l / 8. Numbers and scales of the next batch are asked for
+    // while this one's copies go out (looked up tile by tile they took 1.4 us a tile).
     int C = 0;
     bool go = true;
-    auto look = [&](const CamCursor& w, int tile, float2& sc) {
-      const int p = tile * CAM_PAGES + lane;
-      const int page = lane < CAM_PAGES && tile < min(w.tile1, w.cached) && p * CACHE_PAGE < w.n ? c.page(w.s, p) : -1;
-      sc = make_float2(0.f, 0.f);
-      if (page >= 0) sc = *reinterpret_cast<const float2*>(c.scales + ((layer_heads + w.kvh) * c.n_pages + page) * 2);
-      return page;
+    CamCursor w = u;                             // the batch after: tiles w.tile .. of its unit
+    auto settle = [&]() {                        // to a unit that has cached tiles left; false: none
+      while (w.tile >= min(w.tile1, w.cached))
+        if (!list.next(w)) return false;
+      return true;
     };
-    do {
-      float2 sc, sc_next;
-      int page = look(u, u.tile, sc);
-      for (int tile = u.tile; tile < min(u.tile1, u.cached) && go; ++tile, ++C) {
+    auto look = [&]() {
+      const int tile = w.tile + (lane >> 3), p = tile * CAM_PAGES + (lane & 7);
+      return tile < min(w.tile1, w.cached) && p * CACHE_PAGE < w.n ? c.page(w.s, p) : -1;
+    };
+    auto scales_of = [&](const CamCursor& v, int page) {
+      return page >= 0 ? *reinterpret_cast<const float2*>(c.scales + ((layer_heads + v.kvh) * c.n_pages + page) * 2) : make_float2(0.f, 0.f);
+    };
+    bool more = settle();
+    int page = more ? look() : -1;
+    float2 sc = scales_of(w, page);
+    while (more && go) {
+      const CamCursor now = w;
+      const int count = min(4, min(now.tile1, now.cached) - now.tile);
+      w.tile += count;
+      more = settle();
+      const int page_next = more ? look() : -1;
+      float2 sc_next = make_float2(0.f, 0.f);
+      const float v = sc.y > 0.f ? sc.y * code_unit<FMT>() : 9.094947017729282e-13f;    // (a block of zeros: 2^-40 does not raise the reference)
+      const float2 k = make_float2(sc.x * code_unit<FMT>() * a.scale * 1.44269504088896f, __log2f(v));
+      const uint8_t* src = c.codes + ((layer_heads + now.kvh) * c.n_pages + max(page, 0)) * (2 * (size_t)BLOCK);
+      const uint32_t valid = __ballot_sync(0xffffffffu, page >= 0);
+      for (int t = 0; t < count && go; ++t, ++C) {
         const int cs = C % CS;
-        const int page_next = look(u, tile + 1, sc_next);
         if (C >= CS) go = mbar_wait(code_empty + cs, ((C / CS) - 1) & 1, status, 301);
         if (!__all_sync(0xffffffffu, go)) { go = false; break; }
-        const float v = sc.y > 0.f ? sc.y * code_unit<FMT>() : 9.094947017729282e-13f;    // (a block of zeros: 2^-40 does not raise the reference)
-        if (lane < CAM_PAGES) consts[C & 7][lane] = make_float2(sc.x * code_unit<FMT>() * a.scale * 1.44269504088896f, __log2f(v));
-        const uint32_t valid = __ballot_sync(0xffffffffu, page >= 0);
-        if (lane == 0) mbar_expect_tx(code_full + cs, __popc(valid) * 2 * BLOCK);
+        if (lane >> 3 == t) consts[C & 7][lane & 7] = k;
+        if (lane == 0) mbar_expect_tx(code_full + cs, __popc((valid >> (8 * t)) & 0xff) * 2 * BLOCK);
         __syncwarp();
-        if (page >= 0) bulk_load_1d(code_s + (size_t)cs * 256 * D + lane * 2 * BLOCK, c.codes + ((layer_heads + u.kvh) * c.n_pages + page) * (2 * (size_t)BLOCK), 2 * BLOCK, code_full + cs);
-        page = page_next;
-        sc = sc_next;
+        if (lane >> 3 == t && page >= 0) bulk_load_1d(code_s + (size_t)cs * 256 * D + (lane & 7) * 2 * BLOCK, src, 2 * BLOCK, code_full + cs);
+        if (t == count - 1 || t == 1) sc_next = scales_of(w, page_next);
       }
-    } while (go && list.next(u));
+      page = page_next;
+      sc = sc_next;
+    }
     // (copies still in flight: the last of each stage)
     if (!go)
       for (int x = max(0, C - CS); x < C; ++x) mbar_wait(code_full + x % CS, (x / CS) & 1, status, 302);
@@ -196,15 +236,19 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
-    constexpr int CT = CU_CONV * 32, CHUNKS = CAM_PAGES * D;   // 16-byte chunks of a tile's K, or V
-    auto widen = [&](const uint4& w, uint8_t* row, int j, int x) {     // 16 codes to 16-byte chunks j and j + 1 of a 128-byte row, swizzled by x
+    // A thread has the same 16-byte chunk of every page (D = 64: of every other one), so that its places in the operands differ by constants: chunk y of a K block is token
+    // (y / (D / 2)) * 8 + y % 8, dims 16 (y / 8 % (D / 16)) .. + 15; chunk y of a V block is dim y.
+    constexpr int CT = CU_CONV * 32, PPI = CT / D, ITER = CAM_PAGES / PPI;
+    const int cy = ct % D, cp = ct / D, kch = (cy >> 3) % (D / 16), kx = cy & 7;
+    const uint32_t k_at = (kch >> 2) * 16384 + (cp * 16 + (cy / (D / 2)) * 8 + kx) * 128, k_c0 = (((kch & 3) * 2) ^ kx) << 4, k_c1 = k_c0 ^ 16, v_at = cy * 128;
+    auto widen = [&](const uint4& w, uint8_t* lo, uint8_t* hi) {       // 16 codes to two 16-byte chunks
       uint32_t o[8];
       codes_to<FMT, T>(w.x, o[0], o[1]);
       codes_to<FMT, T>(w.y, o[2], o[3]);
       codes_to<FMT, T>(w.z, o[4], o[5]);
       codes_to<FMT, T>(w.w, o[6], o[7]);
-      *reinterpret_cast<uint4*>(row + ((j ^ x) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-      *reinterpret_cast<uint4*>(row + (((j + 1) ^ x) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+      *reinterpret_cast<uint4*>(lo) = make_uint4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<uint4*>(hi) = make_uint4(o[4], o[5], o[6], o[7]);
     };
     int gt = 0, C = 0, U = 0;
     bool go = true;
@@ -222,6 +266,8 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
         cp_async_commit();
         return true;
       };
+      bool q_asked = U == 0;
+      if (q_asked) ask_q();                 // (later units: behind their first K, when the room is free)
       if (ct == 0) odd[(U + 4) & 7] = 0;    // (no unit that is still worked on: the roles are at most three apart)
       for (int tile = u.tile; tile < u.tile1; ++tile, ++gt) {
         const int st = gt & 1;
@@ -232,20 +278,34 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           go = mbar_wait(code_full + cs, (C / CS) & 1, status, 309) && (gt < 1 || mbar_wait(k_empty, (gt - 1) & 1, status, 310));
           if (!go) break;
           const uint4* codes = reinterpret_cast<const uint4*>(code_s + (size_t)cs * 256 * D);
-#pragma unroll 3
-          for (int x = ct; x < CHUNKS; x += CT) {
-            const int p = x / D, y = x % D, ch = (y >> 3) % (D / 16), key = p * 16 + (y / (D / 2)) * 8 + (y & 7);
-            widen(codes[p * (2 * D) + y], k_s + (ch >> 2) * 16384 + key * 128, (ch & 3) * 2, key & 7);
+#pragma unroll
+          for (int i0 = 0; i0 < ITER; i0 += 4) {
+            uint4 w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = codes[((i0 + i) * PPI + cp) * (2 * D) + cy];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) widen(w[i], k_s + k_at + k_c0 + (i0 + i) * PPI * 2048, k_s + k_at + k_c1 + (i0 + i) * PPI * 2048);
           }
           tell(k_full);
-          if (first && !ask_q()) { go = false; break; }
-          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 311)) { go = false; break; }
-#pragma unroll 3
-          for (int x = ct; x < CHUNKS; x += CT) {
-            const int p = x / D, d = x % D;
-            widen(codes[p * (2 * D) + D + d], v_s + (p >> 2) * (D * 128) + d * 128, (p & 3) * 2, d & 7);
+          if (first && !q_asked && !ask_q()) { go = false; break; }
+          if (first && q_asked) {
+            cp_async_wait<0>();
+            tell(q_full);
           }
-          if (first) {
+          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 311)) { go = false; break; }
+#pragma unroll
+          for (int i0 = 0; i0 < ITER; i0 += 4) {
+            uint4 w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = codes[((i0 + i) * PPI + cp) * (2 * D) + D + cy];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int p = (i0 + i) * PPI + cp, ch = (((p & 3) * 2) ^ kx) << 4;
+              uint8_t* row = v_s + v_at + (p >> 2) * (D * 128);
+              widen(w[i], row + ch, row + (ch ^ 16));
+            }
+          }
+          if (first && !q_asked) {
             cp_async_wait<0>();
             tell(q_full);
           }
@@ -266,7 +326,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           };
           if (gt >= 1 && !mbar_wait(k_empty, (gt - 1) & 1, status, 312)) { go = false; break; }
           copy(a.k, a.k_row, a.k_head, k_s);
-          if (first && !ask_q()) { go = false; break; }
+          if (first && !q_asked && !ask_q()) { go = false; break; }
           if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 313)) { go = false; break; }
           copy(a.v, a.v_row, a.v_head, v_s);
           cp_async_wait<1>();
@@ -340,75 +400,88 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
         for (int x = 0; x < NC; ++x) mine = mine && vis[x] == 0xffffffffu;
         const bool whole = __all_sync(0xffffffffu, mine);
         const float2* pg = consts[(C0 + t) & 7] + kh * 4;
-        float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < NC; ++x) {
+          // 32 keys: two pages, or rows of the pass (their weights w' / c are 2^(z - reference): c counts for the reference alone)
           uint32_t r[32];
           tmem_ld32(s_addr + x * 32, r);
-          tmem_ld_wait();
-          if (!whole)
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!((vis[x] >> j) & 1)) r[j] = 0xff800000u;
-          float m0 = -INFINITY, m1 = -INFINITY;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            m0 = fmaxf(m0, __uint_as_float(r[j]));
-            m1 = fmaxf(m1, __uint_as_float(r[16 + j]));
-          }
-          if (is_new) {
-            top = fmaxf(top, fmaf(fmaxf(m0, m1), scale2, lgc));
-          } else {
-            const float2 k0 = pg[2 * x], k1 = pg[2 * x + 1];
-            top = fmaxf(top, fmaxf(fmaf(m0, k0.x, k0.y), fmaf(m1, k1.x, k1.y)));    // (a page of scale 0 without a key to see gives NaN, which the maximum leaves out)
-          }
-        }
-        const bool raise = top > m_ref + CU_RAISE || (m_ref == -INFINITY && top > -INFINITY);
-        const float m_new = raise ? top : m_ref, alpha = raise ? ex2(m_ref - m_new) : 1.f;
-        if (__any_sync(0xffffffffu, raise && my_tiles > 0)) {
-          const uint32_t o_addr = tmem + lane_base + 256u + grp * 128;
-#pragma unroll 1
-          for (int x = 0; x < D / 32; ++x) {
-            uint32_t r[32];
-            tmem_ld32(o_addr + x * 32, r);
-            tmem_ld_wait();
-#pragma unroll
-            for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * alpha);
-            tmem_st32(o_addr + x * 32, r);
-          }
-        }
-        m_ref = m_new;
-        l_run *= alpha;
-        const float base = m_ref == -INFINITY ? 0.f : m_ref;
-#pragma unroll
-        for (int x = 0; x < NC; ++x) {
-          uint32_t r[32], pk[16];
-          tmem_ld32(s_addr + x * 32, r);
-          float f[2] = {scale2, scale2}, off[2] = {-base, -base}, inv[2] = {1.f, 1.f};
+          float f[2] = {scale2, scale2}, lg[2] = {0.f, 0.f}, inv[2] = {1.f, 1.f};
           if (!is_new) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const float2 k = pg[2 * x + h];
               f[h] = k.x;
-              off[h] = k.y - base;
+              lg[h] = k.y;
               inv[h] = ex2(-k.y);
             }
           }
           tmem_ld_wait();
-          float w[32];
+          float w[32], s0, s1;
+          auto weigh = [&]() {                        // (no reference yet: a key that is seen weighs infinity)
+            const unsigned long long fa = pair2(f[0], f[0]), fb = pair2(f[1], f[1]), oa = pair2(lg[0] - m_ref, lg[0] - m_ref), ob = pair2(lg[1] - m_ref, lg[1] - m_ref);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) w[j] = ex2(fmaf(__uint_as_float(r[j]), f[j >> 4], off[j >> 4]));
-          if (!whole)
+            for (int j = 0; j < 32; j += 2) {
+              const float2 y = fma2(pair2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), j < 16 ? fa : fb, j < 16 ? oa : ob);
+              w[j] = ex2(y.x);
+              w[j + 1] = ex2(y.y);
+            }
+            if (!whole)
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (!((vis[x] >> j) & 1)) w[j] = 0.f;
-          float s0 = 0.f, s1 = 0.f;
+              for (int j = 0; j < 32; ++j)
+                if (!((vis[x] >> j) & 1)) w[j] = 0.f;
+            unsigned long long a0 = pair2(w[0], w[1]), a1 = pair2(w[16], w[17]);
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            s0 += w[j];
-            s1 += w[16 + j];
+            for (int j = 2; j < 16; j += 2) {
+              a0 = add2(a0, pair2(w[j], w[j + 1]));
+              a1 = add2(a1, pair2(w[16 + j], w[17 + j]));
+            }
+            const float2 b0 = unpair2(a0), b1 = unpair2(a1);
+            s0 = b0.x + b0.y;
+            s1 = b1.x + b1.y;
+          };
+          weigh();
+          if (__any_sync(0xffffffffu, fmaxf(s0, s1) * (is_new ? cv : 1.f) > cu_raise<T>())) {
+            // The reference goes up to the largest of these keys; O, the sum and the tile's weights so far are multiplied by what it rose by.
+            float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              if ((vis[x] >> j) & 1) m0 = fmaxf(m0, __uint_as_float(r[j]));
+              if ((vis[x] >> (16 + j)) & 1) m1 = fmaxf(m1, __uint_as_float(r[16 + j]));
+            }
+            // (a page of scale 0 without a key to see gives NaN, which the maximum leaves out)
+            const float top = fmaxf(fmaf(m0, f[0], is_new ? lgc : lg[0]), fmaf(m1, f[1], is_new ? lgc : lg[1]));
+            const float m_new = fmaxf(m_ref, top), alpha = m_new > m_ref ? ex2(m_ref - m_new) : 1.f;
+            m_ref = m_new;
+            l_run *= alpha;
+            if (my_tiles > 0) {
+              const uint32_t o_addr = tmem + lane_base + 256u + grp * 128;
+#pragma unroll 1
+              for (int y = 0; y < D / 16; ++y) {
+                uint32_t q[16];
+                tmem_ld16(o_addr + y * 16, q);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) q[j] = __float_as_uint(__uint_as_float(q[j]) * alpha);
+                tmem_st16(o_addr + y * 16, q);
+              }
+            }
+#pragma unroll 1
+            for (int y = 0; y < x; ++y) {
+              uint32_t q[16];
+              tmem_st_wait();
+              tmem_ld16(p_addr + y * 16, q);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const float2 e = unpack2<T>(q[j]);
+                q[j] = pack2<T>(e.x * alpha, e.y * alpha);
+              }
+              tmem_st16(p_addr + y * 16, q);
+            }
+            weigh();
           }
           l_run += s0 * inv[0] + s1 * inv[1];
+          uint32_t pk[16];
           if (is_new) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) pk[j] = pack2<T>(w[2 * j], w[2 * j + 1]);
@@ -472,6 +545,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       // The room of q, which has been read, serves for what the threads tell one another and for turning rows: a thread has a row, a warp writes out whole rows.
       const uint32_t o_addr = tmem + lane_base + 256u;
       float f0 = 1.f, f1 = 0.f, top = m_ref, sum = l_run;
+      float2 e = make_float2(-INFINITY, 0.f);
       bool has0 = true, has1 = false;
       if constexpr (ALT) {
         // both groups' sums of the row lie in its lane
@@ -479,6 +553,12 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
         ml[grp * 128 + mrow] = make_float2(m_ref, l_run);
         softmax_bar();
         const float2 e0 = ml[mrow], e1 = ml[128 + mrow];
+        if constexpr (ROWS == 64) {                             // the row's other half
+          const float2 h0 = ml[mrow ^ 64], h1 = ml[128 + (mrow ^ 64)];
+          e.x = fmaxf(h0.x, h1.x);
+          const float hr = e.x == -INFINITY ? 0.f : e.x;
+          e.y = ex2(h0.x - hr) * h0.y + ex2(h1.x - hr) * h1.y;
+        }
         softmax_bar();                                          // (all have read: values come over it)
         top = fmaxf(e0.x, e1.x);
         const float ref = top == -INFINITY ? 0.f : top;
@@ -510,36 +590,43 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
         }
       };
       if constexpr (ROWS == 64) {
-        // a group has half of the dims; the second half's sums go over to the threads of the first: [64][D], 16-byte chunk x of row r at x ^ (r % 8)
+        // Thread (group, key half, row) finishes a quarter of the row's dims: the other half's thread of the same group and row hands that quarter over and gets one in turn
+        // ([64][D], 16-byte chunk x of row r at x ^ (r % 8)).
+        static_assert(D % 64 == 0, "quarters of at least 16 dims");
+        constexpr int DQ = D / 4;
         float* xb = reinterpret_cast<float*>(q_s) + qrow * D;
-        constexpr int DH = D / 2;
-        if (kh == 1) {
-          if (grp == 0) xm[qrow] = make_float2(top, sum);
-#pragma unroll 1
-          for (int x = 0; x < DH; x += 32) {
-            float v[32];
-            load(grp * DH + x, v);
+        const int mine_at = (grp * 2 + kh) * DQ, theirs_at = (grp * 2 + (kh ^ 1)) * DQ;
+        auto load_quarter = [&](int col, float (&v)[DQ]) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(xb + ((((grp * DH + x + j) >> 2) ^ (qrow & 7)) << 2)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          for (int h = 0; h < DQ; h += 16) {
+            uint32_t r0[16], r1[16];
+            __syncwarp();
+            tmem_ld16(o_addr + col + h, r0);
+            tmem_ld16(o_addr + 128 + col + h, r1);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[h + j] = (has0 ? f0 * __uint_as_float(r0[j]) : 0.f) + (has1 ? f1 * __uint_as_float(r1[j]) : 0.f);
           }
+        };
+        {
+          float v[DQ];
+          load_quarter(theirs_at, v);
+#pragma unroll
+          for (int j = 0; j < DQ; j += 4) *reinterpret_cast<float4*>(xb + ((((theirs_at + j) >> 2) ^ (qrow & 7)) << 2)) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
         }
         softmax_bar();
-        if (kh == 0) {
-          const float2 e = xm[qrow];
-          const float t2 = fmaxf(top, e.x), rf = t2 == -INFINITY ? 0.f : t2, s2 = ex2(top - rf) * sum + ex2(e.x - rf) * e.y;
-          const float k = grp == 0 ? head(t2, s2) : !whole_unit ? 1.f : s2 > 0.f || s2 != s2 ? 1.f / s2 : 0.f, g0 = k * ex2(top - rf), g1 = k * ex2(e.x - rf);
-#pragma unroll 1
-          for (int x = 0; x < DH; x += 32) {
-            float v[32];
-            load(grp * DH + x, v);
+        {
+          const float t2 = fmaxf(top, e.x), rf = t2 == -INFINITY ? 0.f : t2, w0 = ex2(top - rf), w1 = ex2(e.x - rf), s2 = w0 * sum + w1 * e.y;
+          const float k = grp == 0 && kh == 0 ? head(t2, s2) : !whole_unit ? 1.f : s2 > 0.f || s2 != s2 ? 1.f / s2 : 0.f, g0 = k * w0, g1 = k * w1;
+          float v[DQ];
+          load_quarter(mine_at, v);
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              float4* at = reinterpret_cast<float4*>(xb + ((((grp * DH + x + j) >> 2) ^ (qrow & 7)) << 2));
-              const float4 y = *at;
-              float4 w = make_float4(g0 * v[j] + g1 * y.x, g0 * v[j + 1] + g1 * y.y, g0 * v[j + 2] + g1 * y.z, g0 * v[j + 3] + g1 * y.w);
-              if (any_odd && live) add_odd(grp * DH + x + j, w);
-              *at = w;
-            }
+          for (int j = 0; j < DQ; j += 4) {
+            float4* at = reinterpret_cast<float4*>(xb + ((((mine_at + j) >> 2) ^ (qrow & 7)) << 2));
+            const float4 y = *at;
+            float4 w = make_float4(g0 * v[j] + g1 * y.x, g0 * v[j + 1] + g1 * y.y, g0 * v[j + 2] + g1 * y.z, g0 * v[j + 3] + g1 * y.w);
+            if (any_odd && live) add_odd(mine_at + j, w);
+            *at = w;
           }
         }
         softmax_bar();
