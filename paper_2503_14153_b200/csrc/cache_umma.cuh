@@ -3,7 +3,7 @@
 //
 // A CTA has ROWS = 64, 128 or 256 (row, head) rows of one (sequence, kv head) and takes its run of tiles of 128 keys:
 //   producer warp     brings a tile's pages (K and V of a page are one block) with bulk copies, 8 a tile, one a lane;
-//   4 converter warps turn codes into operands of the query's type: a 16-byte row of a core matrix (16 dims of a token, 16 tokens of a dim) becomes two 16-byte
+//   6 converter warps, three for K and three for V, turn codes into operands of the query's type: a 16-byte row of a core matrix (16 dims of a token, 16 tokens of a dim) becomes two 16-byte
 //                     chunks of a 128-byte-swizzled K-major tile, so K [128 keys][D] and V^T [D][128 keys] need no transpose; rows of the pass are copied (V as it is: MN-major);
 //   one thread        issues S = Q K^T and O += P V;
 //   8 softmax warps   in two groups, a thread a row: S out of tensor memory, weights back into the same columns as the A operand of P V.
@@ -16,17 +16,17 @@
 
 namespace spec {
 
-constexpr int CU_SOFT = 8, CU_CONV = 4;                       // softmax and converter warps
-constexpr int CU_WARPS = CU_SOFT + CU_CONV + 2, CU_THREADS = 32 * CU_WARPS;
+constexpr int CU_SOFT = 8, CU_SIDE = 3, CU_CONV = 2 * CU_SIDE;   // softmax warps; converter warps of K, or of V
+constexpr int CU_WARPS = CU_SOFT + CU_CONV + 2, CU_THREADS = 32 * CU_WARPS;   // four warps an SM quarter: 128 registers a thread
 constexpr int CU_PAIRS = 256;                                 // (sequence, row tile) pairs a launch can deal
 constexpr int CU_NEW = 128;                                   // rows of the pass a tile
 // What 16 keys may weigh together before the reference is raised. bf16 weights and float32 sums lose nothing at any size (raising at 128: 313 us for a prompt that takes 250); float16 weights, up to
 // 2^7 times this with the rows of the pass, stay below 2^15.
 template <typename T> __host__ __device__ constexpr float cu_raise() { return std::is_same<T, bf16>::value ? 1.1529215046068470e18f : 256.f; }
 
-__host__ __device__ constexpr int cu_code_stages(int ROWS) { return ROWS == 256 ? 2 : 3; }
+__host__ __device__ constexpr int cu_v_stages(int ROWS) { return ROWS == 256 ? 1 : 2; }
 __host__ __device__ constexpr size_t cu_smem(int D, int ROWS) {
-  return 1024 + (size_t)(ROWS == 256 ? 2 : 1) * 128 * D * 2 /*Q*/ + 3 * (size_t)(128 * D * 2) /*K, two of V*/ + (size_t)cu_code_stages(ROWS) * 256 * D /*codes*/;
+  return 1024 + (size_t)((ROWS == 256 ? 2 : 1) /*Q*/ + 2 /*K*/ + cu_v_stages(ROWS)) * 128 * D * 2 + 2 * (size_t)256 * D /*codes*/;
 }
 
 // D[tmem] (+)= A[tmem] * B[smem]
@@ -70,7 +70,7 @@ __device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigne
 
 template <typename T, int D, int FMT, int ROWS>
 __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnArgs a, CamPlan pl) {
-  constexpr int CS = cu_code_stages(ROWS), BLOCK = CACHE_PAGE * D, OPER = 128 * D * 2;   // OPER: bytes of one operand tile (Q, K or V)
+  constexpr int CS = 2, VS = cu_v_stages(ROWS), BLOCK = CACHE_PAGE * D, OPER = 128 * D * 2;   // OPER: bytes of one operand tile (Q, K or V)
   constexpr int NQ = ROWS == 256 ? 2 : 1;
   constexpr bool ALT = ROWS != 256;                            // the groups take alternate tiles
   extern __shared__ uint8_t smem_raw[];
@@ -80,10 +80,10 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   __shared__ uint32_t tmem_slot;
   const uint32_t raw = smem_u32(smem_raw);
   uint8_t* q_s = smem_raw + (((raw + 1023u) & ~1023u) - raw);
-  uint8_t* k_s = q_s + NQ * OPER;
-  uint8_t* v_s0 = k_s + OPER;                                  // [2]
-  uint8_t* code_s = v_s0 + 2 * OPER;                           // [CS]
-  uint64_t *code_full = bars, *code_empty = bars + 3, *k_full = bars + 6, *k_empty = bars + 7, *v_full = bars + 8, *v_empty = bars + 10, *s_full = bars + 12, *p_full = bars + 14, *q_full = bars + 16,
+  uint8_t* k_s0 = q_s + NQ * OPER;                             // [2]
+  uint8_t* v_s0 = k_s0 + 2 * OPER;                             // [VS]
+  uint8_t* code_s = v_s0 + VS * OPER;                          // [CS]
+  uint64_t *code_full = bars, *code_empty = bars + 2, *k_full = bars + 4, *k_empty = bars + 6, *v_full = bars + 8, *v_empty = bars + 10, *s_full = bars + 12, *p_full = bars + 14, *q_full = bars + 16,
            *q_empty = bars + 17, *o_full = bars + 18;
   const CacheView& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.H / c.kv;
@@ -94,20 +94,18 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   CamCursor u;
   if (!list.first(u)) return;
   if (tid == 0) {
-    for (int i = 0; i < CS; ++i) {
+    for (int i = 0; i < 2; ++i) {
       mbar_init(code_full + i, 1);
       mbar_init(code_empty + i, CU_CONV);
-    }
-    mbar_init(k_full, CU_CONV);
-    mbar_init(k_empty, 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(v_full + i, CU_CONV);
+      mbar_init(k_full + i, CU_SIDE);
+      mbar_init(k_empty + i, 1);
+      mbar_init(v_full + i, CU_SIDE);
       mbar_init(v_empty + i, 1);
       mbar_init(s_full + i, 1);
       mbar_init(p_full + i, 4);
     }
     for (int i = 0; i < 8; ++i) odd[i] = 0;
-    mbar_init(q_full, CU_CONV);
+    mbar_init(q_full, CU_SIDE);
     mbar_init(q_empty, 1 + CU_SOFT);
     mbar_init(o_full, 1);
     mbar_fence_init();
@@ -183,22 +181,23 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
         const int nt = u.tile1 - u.tile;
         auto mma_s = [&](int t, int x) {           // scores of tile t; x: S buffer and, with 256 rows, Q tile
           if (t == 0 && x == (ALT ? (T0 & 1) : 0) && !mbar_wait(q_full, U & 1, status, 303)) return false;
-          if (!mbar_wait(k_full, (T0 + t) & 1, status, 304)) return false;
+          const int ks = (T0 + t) & 1;
+          if (!mbar_wait(k_full + ks, ((T0 + t) >> 1) & 1, status, 304)) return false;
           tc_fence_after();
-          const uint32_t k_addr = smem_u32(k_s), qa = q_addr + (ALT ? 0 : x * OPER);
+          const uint32_t k_addr = smem_u32(k_s0 + ks * OPER), qa = q_addr + (ALT ? 0 : x * OPER);
 #pragma unroll
           for (int j = 0; j < D / 16; ++j)
             tc_mma_f16(tmem + x * 128, make_kmajor_sw128_desc(qa + (j >> 2) * 16384) + 2 * (j & 3), make_kmajor_sw128_desc(k_addr + (j >> 2) * 16384) + 2 * (j & 3), idesc_s, j > 0);
           tc_commit(s_full + x);
           if (ALT || x == 1) {
-            tc_commit(k_empty);
+            tc_commit(k_empty + ks);
             if (t == nt - 1) tc_commit(q_empty);
           }
           return true;
         };
         auto mma_o = [&](int t, int x, bool first) {
-          const int gt = T0 + t, st = gt & 1;
-          if (!mbar_wait(p_full + x, (ALT ? gt >> 1 : gt) & 1, status, 305) || !mbar_wait(v_full + st, (gt >> 1) & 1, status, 306)) return false;
+          const int gt = T0 + t, st = gt % VS;
+          if (!mbar_wait(p_full + x, (ALT ? gt >> 1 : gt) & 1, status, 305) || !mbar_wait(v_full + st, (gt / VS) & 1, status, 306)) return false;
           tc_fence_after();
           const uint32_t v_addr = smem_u32(v_s0 + st * OPER);
           const bool is_new = u.tile + t >= u.cached;
@@ -229,123 +228,118 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
     }
     __syncwarp();
   } else if (warp >= CU_SOFT) {
-    // ---- converters
-    const int ct = tid - CU_SOFT * 32;
+    // ---- converters: three warps for K (and q), three for V, at their own pace. A warp takes 32 rows of 16 bytes at a time, CU_SIDE warps in turn; piece `it` of a tile is page
+    // it / PER, part it % PER of its block. Lane l has token l % 8, 16-dim chunk l / 8 of a piece of K, dim l of a piece of V, so that its places in the operand differ by constants.
+    constexpr int PER = D / 32, PIECES = CAM_PAGES * PER;
+    const int side = (warp - CU_SOFT) / CU_SIDE, w = (warp - CU_SOFT) % CU_SIDE, ct = w * 32 + lane, CT = CU_SIDE * 32;
+    const uint32_t x8 = lane & 7;
     auto tell = [&](uint64_t* bar) {               // what this warp's threads wrote may be read by the tensor cores
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
-    // A thread has the same 16-byte chunk of every page (D = 64: of every other one), so that its places in the operands differ by constants: chunk y of a K block is token
-    // (y / (D / 2)) * 8 + y % 8, dims 16 (y / 8 % (D / 16)) .. + 15; chunk y of a V block is dim y.
-    constexpr int CT = CU_CONV * 32, PPI = CT / D, ITER = CAM_PAGES / PPI;
-    const int cy = ct % D, cp = ct / D, kch = (cy >> 3) % (D / 16), kx = cy & 7;
-    const uint32_t k_at = (kch >> 2) * 16384 + (cp * 16 + (cy / (D / 2)) * 8 + kx) * 128, k_c0 = (((kch & 3) * 2) ^ kx) << 4, k_c1 = k_c0 ^ 16, v_at = cy * 128;
-    auto widen = [&](const uint4& w, uint8_t* lo, uint8_t* hi) {       // 16 codes to two 16-byte chunks
+    auto widen = [&](const uint4& c4, uint8_t* lo, uint8_t* hi) {      // 16 codes to two 16-byte chunks
       uint32_t o[8];
-      codes_to<FMT, T>(w.x, o[0], o[1]);
-      codes_to<FMT, T>(w.y, o[2], o[3]);
-      codes_to<FMT, T>(w.z, o[4], o[5]);
-      codes_to<FMT, T>(w.w, o[6], o[7]);
+      codes_to<FMT, T>(c4.x, o[0], o[1]);
+      codes_to<FMT, T>(c4.y, o[2], o[3]);
+      codes_to<FMT, T>(c4.z, o[4], o[5]);
+      codes_to<FMT, T>(c4.w, o[6], o[7]);
       *reinterpret_cast<uint4*>(lo) = make_uint4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<uint4*>(hi) = make_uint4(o[4], o[5], o[6], o[7]);
+    };
+    // rows of the pass, 128 of them and zeros past the last one: [128 rows][64 dims] slabs, 16-byte chunk ch of row r at chunk ch ^ (r % 8) of its 128 bytes
+    auto copy = [&](const void* base, long long row_stride, long long head_stride, uint8_t* to, int j0) {
+      for (int x = ct; x < 128 * (D / 8); x += CT) {
+        const int r = x / (D / 8), ch = x % (D / 8);
+        const bool in = j0 + r < u.R;
+        const T* src = static_cast<const T*>(base) + (long long)(u.r0 + (in ? j0 + r : 0)) * row_stride + (long long)u.kvh * head_stride + ch * 8;
+        cp_async16(smem_u32(to) + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4), src, in ? 16 : 0);
+      }
+      cp_async_commit();
     };
     int gt = 0, C = 0, U = 0;
     bool go = true;
     do {
-      const int rtile = pl.rt0 + u.rt;
-      // q: row r of the tile at row r (64 rows: and at r + 64), 16-byte chunk ch at chunk ch ^ (r % 8) of its 128 bytes. Its room is free when the last unit's output is through.
-      auto ask_q = [&]() {
-        if (U > 0 && !mbar_wait(q_empty, (U - 1) & 1, status, 308)) return false;
-        for (int x = ct; x < NQ * 128 * (D / 8); x += CT) {
-          const int r = x / (D / 8), ch = x % (D / 8), m = rtile * ROWS + (ROWS == 64 ? r & 63 : r), i = m / G;
-          const bool live = i < u.R;
-          const T* src = static_cast<const T*>(a.q) + (long long)(u.r0 + (live ? i : 0)) * a.q_row + (long long)(u.kvh * G + (live ? m - i * G : 0)) * a.q_head + ch * 8;
-          cp_async16(smem_u32(q_s) + (r >> 7) * OPER + (ch >> 3) * 16384 + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4), src, live ? 16 : 0);
-        }
-        cp_async_commit();
-        return true;
-      };
-      bool q_asked = U == 0;
-      if (q_asked) ask_q();                 // (later units: behind their first K, when the room is free)
-      if (ct == 0) odd[(U + 4) & 7] = 0;    // (no unit that is still worked on: the roles are at most three apart)
-      for (int tile = u.tile; tile < u.tile1; ++tile, ++gt) {
-        const int st = gt & 1;
-        const bool first = tile == u.tile;
-        uint8_t* v_s = v_s0 + st * OPER;
-        if (tile < u.cached) {
-          const int cs = C % CS;
-          go = mbar_wait(code_full + cs, (C / CS) & 1, status, 309) && (gt < 1 || mbar_wait(k_empty, (gt - 1) & 1, status, 310));
+      if (side == 0) {
+        // q, in the same slabs: row r of the tile at row r (64 rows: and at r + 64). Its room is free when the last unit's output is through.
+        auto ask_q = [&]() {
+          if (U > 0 && !mbar_wait(q_empty, (U - 1) & 1, status, 308)) return false;
+          for (int x = ct; x < NQ * 128 * (D / 8); x += CT) {
+            const int r = x / (D / 8), ch = x % (D / 8), m = (pl.rt0 + u.rt) * ROWS + (ROWS == 64 ? r & 63 : r), i = m / G;
+            const bool live = i < u.R;
+            const T* src = static_cast<const T*>(a.q) + (long long)(u.r0 + (live ? i : 0)) * a.q_row + (long long)(u.kvh * G + (live ? m - i * G : 0)) * a.q_head + ch * 8;
+            cp_async16(smem_u32(q_s) + (r >> 7) * OPER + (ch >> 3) * 16384 + (r & 127) * 128 + (((ch & 7) ^ (r & 7)) << 4), src, live ? 16 : 0);
+          }
+          cp_async_commit();
+          return true;
+        };
+        if (U == 0) ask_q();                         // (later units: behind their first K, when the room is free)
+        const uint32_t c0 = (((lane >> 3) * 2) ^ x8) << 4, c1 = c0 ^ 16;
+        for (int tile = u.tile; tile < u.tile1; ++tile, ++gt) {
+          uint8_t* k_s = k_s0 + (gt & 1) * OPER;
+          const bool cached = tile < u.cached;
+          go = (!cached || mbar_wait(code_full + C % CS, (C / CS) & 1, status, 309)) && (gt < 2 || mbar_wait(k_empty + (gt & 1), ((gt >> 1) - 1) & 1, status, 310));
           if (!go) break;
-          const uint4* codes = reinterpret_cast<const uint4*>(code_s + (size_t)cs * 256 * D);
-#pragma unroll
-          for (int i0 = 0; i0 < ITER; i0 += 4) {
-            uint4 w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = codes[((i0 + i) * PPI + cp) * (2 * D) + cy];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) widen(w[i], k_s + k_at + k_c0 + (i0 + i) * PPI * 2048, k_s + k_at + k_c1 + (i0 + i) * PPI * 2048);
-          }
-          tell(k_full);
-          if (first && !q_asked && !ask_q()) { go = false; break; }
-          if (first && q_asked) {
-            cp_async_wait<0>();
-            tell(q_full);
-          }
-          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 311)) { go = false; break; }
-#pragma unroll
-          for (int i0 = 0; i0 < ITER; i0 += 4) {
-            uint4 w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = codes[((i0 + i) * PPI + cp) * (2 * D) + D + cy];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int p = (i0 + i) * PPI + cp, ch = (((p & 3) * 2) ^ kx) << 4;
-              uint8_t* row = v_s + v_at + (p >> 2) * (D * 128);
-              widen(w[i], row + ch, row + (ch ^ 16));
+          if (cached) {
+            const uint4* codes = reinterpret_cast<const uint4*>(code_s + (size_t)(C % CS) * 256 * D) + lane;
+#pragma unroll 4
+            for (int it = w; it < PIECES; it += CU_SIDE) {
+              const int p = it / PER, y = it % PER;
+              uint8_t* row = k_s + (D == 128 ? (y & 1) * 16384 + (y >> 1) * 1024 : y * 1024) + p * 2048 + x8 * 128;
+              widen(codes[p * (2 * D) + y * 32], row + c0, row + c1);
             }
+          } else {
+            copy(a.k, a.k_row, a.k_head, k_s, (tile - u.cached) * CU_NEW);
+            cp_async_wait<0>();
           }
-          if (first && !q_asked) {
+          tell(k_full + (gt & 1));
+          if (cached) {
+            if (lane == 0) mbar_arrive(code_empty + C % CS);
+            ++C;
+          }
+          if (tile == u.tile) {
+            if (U > 0 && !ask_q()) { go = false; break; }
             cp_async_wait<0>();
             tell(q_full);
           }
-          tell(v_full + st);
-          if (lane == 0) mbar_arrive(code_empty + cs);
-          ++C;
-        } else {
-          // rows of the pass: K and V alike [128 rows][64 dims] slabs, zeros past the last row
-          const int j0 = (tile - u.cached) * CU_NEW;
-          auto copy = [&](const void* base, long long row_stride, long long head_stride, uint8_t* to) {
+        }
+      } else {
+        if (ct == 0) odd[(U + 4) & 7] = 0;           // (no unit that is still worked on: the roles are at most three apart)
+        for (int tile = u.tile; tile < u.tile1; ++tile, ++gt) {
+          uint8_t* v_s = v_s0 + gt % VS * OPER;
+          const bool cached = tile < u.cached;
+          go = (!cached || mbar_wait(code_full + C % CS, (C / CS) & 1, status, 311)) && (gt < VS || mbar_wait(v_empty + gt % VS, (gt / VS - 1) & 1, status, 312));
+          if (!go) break;
+          if (cached) {
+            const uint4* codes = reinterpret_cast<const uint4*>(code_s + (size_t)(C % CS) * 256 * D) + D + lane;
+#pragma unroll 4
+            for (int it = w; it < PIECES; it += CU_SIDE) {
+              const int p = it / PER, y = it % PER;
+              uint8_t* row = v_s + (p >> 2) * (D * 128) + (y * 32 + lane) * 128;
+              const uint32_t ch = (((p & 3) * 2) ^ x8) << 4;
+              widen(codes[p * (2 * D) + y * 32], row + ch, row + (ch ^ 16));
+            }
+          } else {
+            copy(a.v, a.v_row, a.v_head, v_s, (tile - u.cached) * CU_NEW);
+            cp_async_wait<0>();
+            // infinities and NaN of V would reach rows that do not see them (0 * NaN): they are taken out here and added at the end, to the rows that do
+            bool found = false;
             for (int x = ct; x < 128 * (D / 8); x += CT) {
               const int r = x / (D / 8), ch = x % (D / 8);
-              const bool in = j0 + r < u.R;
-              const T* src = static_cast<const T*>(base) + (long long)(u.r0 + (in ? j0 + r : 0)) * row_stride + (long long)u.kvh * head_stride + ch * 8;
-              cp_async16(smem_u32(to) + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4), src, in ? 16 : 0);
+              uint4* at = reinterpret_cast<uint4*>(v_s + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4));   // (this thread's own copy)
+              const uint4 v = *at;
+              if (odd2<T>(v.x) || odd2<T>(v.y) || odd2<T>(v.z) || odd2<T>(v.w)) {
+                found = true;
+                *at = make_uint4(tame2<T>(v.x), tame2<T>(v.y), tame2<T>(v.z), tame2<T>(v.w));
+              }
             }
-            cp_async_commit();
-          };
-          if (gt >= 1 && !mbar_wait(k_empty, (gt - 1) & 1, status, 312)) { go = false; break; }
-          copy(a.k, a.k_row, a.k_head, k_s);
-          if (first && !q_asked && !ask_q()) { go = false; break; }
-          if (gt >= 2 && !mbar_wait(v_empty + st, ((gt >> 1) - 1) & 1, status, 313)) { go = false; break; }
-          copy(a.v, a.v_row, a.v_head, v_s);
-          cp_async_wait<1>();
-          tell(k_full);
-          if (first) tell(q_full);
-          cp_async_wait<0>();
-          // infinities and NaN of V would reach rows that do not see them (0 * NaN): they are taken out here and added at the end, to the rows that do
-          bool found = false;
-          for (int x = ct; x < 128 * (D / 8); x += CT) {
-            const int r = x / (D / 8), ch = x % (D / 8);
-            uint4* at = reinterpret_cast<uint4*>(v_s + (ch >> 3) * 16384 + r * 128 + (((ch & 7) ^ (r & 7)) << 4));   // (this thread's own copy)
-            uint4 w = *at;
-            if (odd2<T>(w.x) || odd2<T>(w.y) || odd2<T>(w.z) || odd2<T>(w.w)) {
-              found = true;
-              *at = make_uint4(tame2<T>(w.x), tame2<T>(w.y), tame2<T>(w.z), tame2<T>(w.w));
-            }
+            if (found) odd[U & 7] = 1;
           }
-          if (found) odd[U & 7] = 1;
-          tell(v_full + st);
+          tell(v_full + gt % VS);
+          if (cached) {
+            if (lane == 0) mbar_arrive(code_empty + C % CS);
+            ++C;
+          }
         }
       }
       ++U;

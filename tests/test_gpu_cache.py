@@ -225,6 +225,33 @@ def test_attention_repeats_bit_for_bit_and_on_another_stream(torch):
     assert torch.equal(a, b) and all(torch.equal(a, x) for x in outs)
 
 
+@pytest.mark.parametrize("batch,heads,kv,D,n,rows,mask,fmt", [(1, 32, 32, 128, 2048, 1024, "causal", "int8"), (1, 32, 32, 128, 8192, 64, "tree", "int8"), (1, 32, 8, 128, 4100, 128, "tree", "e4m3"),
+                                                              (3, 16, 4, 64, 3000, 23, "tree", "e4m3"), (1, 16, 4, 64, 0, 1500, "causal", "int8"), (5, 32, 8, 128, 3000, 1, "causal", "int8")])
+def test_attention_many_tiles_a_cta(torch, batch, heads, kv, D, n, rows, mask, fmt):
+    """Passes in which a CTA has many tiles and several units, against the float32 kernel (which the other tests hold to the definition) on the same values."""
+    from paper_2503_14153_b200 import SpecCache
+    rng = np.random.default_rng(n + rows)
+    g = torch.Generator(device="cuda").manual_seed(n + rows)
+    per = -(-n // 16) + 1
+    dev = SpecCache(1, kv, D, batch * per + 3, batch, per, fmt=fmt)
+    lens = [n - 37 * b for b in range(batch)]
+    dev.reserve(_ints(torch, lens))
+    dev.codes.copy_(torch.randint(0, 256, dev.codes.shape, generator=g, device="cuda", dtype=torch.uint8) & (0xff if fmt == "int8" else 0xbf))      # (e4m3: below 2)
+    dev.codes[dev.codes == 0x80] = 0
+    dev.scales.copy_(torch.rand(dev.scales.shape, generator=g, device="cuda") * (0.03 if fmt == "int8" else 2.0) + 1e-3)
+    positive = SpecCache.from_tensors(dev.codes.clone(), dev.scales, dev.page_table, dev.refs, dev.lens, fmt=fmt)
+    positive.codes[:, :, :, 1] = dev.codes[:, :, :, 1].view(torch.int8).abs().view(torch.uint8) if fmt == "int8" else dev.codes[:, :, :, 1] & 0x7f
+    q, k, v = ((torch.randn((batch * rows, h, D), generator=g, device="cuda") * s).bfloat16() for h, s in ((heads, 1.5), (kv, 1.0), (kv, 1.0)))
+    m = _words(torch, [_tree(rng, rows) for _ in range(batch)], -(-rows // 32)) if mask == "tree" else None
+    out, lse = dev.attention(0, q, k, v, batch=batch, mask=m, lse=True)
+    dev.check()
+    want, wl = dev.attention(0, q.float(), k.float(), v.float(), batch=batch, mask=m, lse=True)
+    mass = positive.attention(0, q.float(), k.float(), v.float().abs(), batch=batch, mask=m)
+    # rounding of weights and result to bf16, of scores (up to some tens) and sums to float32 on both sides
+    assert ((out.float() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -7 + 2.0 ** -14) * mass).all()
+    assert ((lse - wl).abs() <= 2.0 ** -14).all()
+
+
 def test_attention_long_cache_past_two_gigabytes(torch):
     # block offsets of more than 2^31 bytes: a pool of 2.3 GB of which the sequence holds the last pages
     from paper_2503_14153_b200 import SpecCache
