@@ -271,7 +271,7 @@ struct CamCursor {
 };
 
 // The list of units as a CTA sees it. MT: rows of a row tile; NEW: rows of the pass a tile; pre: prefix sums over the (sequence, row tile) pairs, in shared memory.
-template <int MT, int NEW> struct CamList {
+template <int MT, int NEW, int UNIT> struct CamList {
   const CacheAttnArgs& a;
   const CamPlan& pl;
   const int* pre;
@@ -304,7 +304,7 @@ template <int MT, int NEW> struct CamList {
         u.b = p / pl.nrt;
         u.rt = p - u.b * pl.nrt;
         fill(a, pl, u);
-        table[p] = u.tiles ? u.tiles + CAM_UNIT : 0;
+        table[p] = u.tiles ? u.tiles + UNIT : 0;
         mine += table[p];
       }
     }
@@ -339,12 +339,12 @@ template <int MT, int NEW> struct CamList {
   }
   __device__ __forceinline__ void enter(CamCursor& u, long long at) const {   // at: a slot of the unit, u.unit0 its first
     fill(a, pl, u);
-    u.tile = max(0, (int)(at - u.unit0) - CAM_UNIT);
-    u.tile1 = (int)min((long long)u.tiles, run1 - u.unit0 - CAM_UNIT);
+    u.tile = max(0, (int)(at - u.unit0) - UNIT);
+    u.tile1 = (int)min((long long)u.tiles, run1 - u.unit0 - UNIT);
   }
   // the next unit of the run that has tiles in it; false when the run is over
   __device__ __forceinline__ bool next(CamCursor& u) const {
-    long long at = u.unit0 + u.tiles + CAM_UNIT;
+    long long at = u.unit0 + u.tiles + UNIT;
     do {
       if (at >= run1) return false;
       do {
@@ -358,7 +358,7 @@ template <int MT, int NEW> struct CamList {
       } while (pre[u.b * pl.nrt + u.rt + 1] == pre[u.b * pl.nrt + u.rt]);
       u.unit0 = at;
       enter(u, at);
-      at += u.tiles + CAM_UNIT;
+      at += u.tiles + UNIT;
     } while (u.tile >= u.tile1);
     return true;
   }
@@ -386,11 +386,11 @@ template <int MT, int NEW> struct CamList {
   // ---- parts of a unit that is cut: where this CTA leaves its own, and who has the others. The first of a unit's CTAs reaches its first tile from before (slot 1), the others begin
   // inside it (slot 0); so a CTA that ends one unit and begins another has a slot for each.
   __device__ __forceinline__ float* part(const CamCursor& u, int D) const {
-    return pl.part + ((size_t)blockIdx.x * 2 + (run0 > u.unit0 + CAM_UNIT ? 0 : 1)) * ((size_t)MT * (D + 2));
+    return pl.part + ((size_t)blockIdx.x * 2 + (run0 > u.unit0 + UNIT ? 0 : 1)) * ((size_t)MT * (D + 2));
   }
   __device__ __forceinline__ const float* part_of(int cta, int c0, int D) const { return pl.part + ((size_t)cta * 2 + (cta == c0 ? 1 : 0)) * ((size_t)MT * (D + 2)); }
-  __device__ __forceinline__ int first_cta(const CamCursor& u) const { return deal.owner(u.unit0 + CAM_UNIT); }
-  __device__ __forceinline__ int last_cta(const CamCursor& u) const { return deal.owner(u.unit0 + CAM_UNIT + u.tiles - 1); }
+  __device__ __forceinline__ int first_cta(const CamCursor& u) const { return deal.owner(u.unit0 + UNIT); }
+  __device__ __forceinline__ int last_cta(const CamCursor& u) const { return deal.owner(u.unit0 + UNIT + u.tiles - 1); }
   __device__ __forceinline__ int* arrive(const CamCursor& u) const { return pl.arrive + ((size_t)u.b * pl.nrt + u.rt) * a.c.kv + u.kvh; }
 };
 
@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
   const int rg = warp % RG, kg = warp / RG;
   const int G = a.H / c.kv;
 
-  CamList<MT, CAM_NEW> list{a, pl};
+  CamList<MT, CAM_NEW, CAM_UNIT> list{a, pl};
   if (!list.template make<CAM_THREADS>(pre, scan)) return;
   CamCursor use;
   if (!list.first(use)) return;

@@ -19,6 +19,7 @@ namespace spec {
 constexpr int CU_SOFT = 8, CU_SIDE = 3, CU_CONV = 2 * CU_SIDE;   // softmax warps; converter warps of K, or of V
 constexpr int CU_WARPS = CU_SOFT + CU_CONV + 2, CU_THREADS = 32 * CU_WARPS;   // four warps an SM quarter: 128 registers a thread
 constexpr int CU_PAIRS = 256;                                 // (sequence, row tile) pairs a launch can deal
+constexpr int CU_UNIT = 4;                                    // a unit's fixed cost, in tiles
 constexpr int CU_NEW = 128;                                   // rows of the pass a tile
 // What 16 keys may weigh together before the reference is raised. bf16 weights and float32 sums lose nothing at any size (raising at 128: 313 us for a prompt that takes 250); float16 weights, up to
 // 2^7 times this with the rows of the pass, stay below 2^15.
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, G = a.H / c.kv;
   int* status = c.status;
 
-  CamList<ROWS, CU_NEW> list{a, pl};
+  CamList<ROWS, CU_NEW, CU_UNIT> list{a, pl};
   if (!list.template make<CU_THREADS>(pre, scan)) return;      // (all threads of the CTA agree, before anything is allocated)
   CamCursor u;
   if (!list.first(u)) return;
@@ -148,6 +149,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       more = settle();
       const int page_next = more ? look() : -1;
       float2 sc_next = make_float2(0.f, 0.f);
+      if (page_next >= 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(c.codes + ((layer_heads + w.kvh) * c.n_pages + page_next) * (2 * (size_t)BLOCK)), "n"(2 * BLOCK) : "memory");
       const float v = sc.y > 0.f ? sc.y * code_unit<FMT>() : 9.094947017729282e-13f;    // (a block of zeros: 2^-40 does not raise the reference)
       const float2 k = make_float2(sc.x * code_unit<FMT>() * a.scale * 1.44269504088896f, __log2f(v));
       const uint8_t* src = c.codes + ((layer_heads + now.kvh) * c.n_pages + max(page, 0)) * (2 * (size_t)BLOCK);
@@ -247,6 +249,23 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       *reinterpret_cast<uint4*>(lo) = make_uint4(o[0], o[1], o[2], o[3]);
       *reinterpret_cast<uint4*>(hi) = make_uint4(o[4], o[5], o[6], o[7]);
     };
+    // the warp's pieces of a tile, four read at a time (piece by piece, a read waits behind the stores before it)
+    auto each_piece = [&](const uint4* codes, auto work) {
+#pragma unroll 1
+      for (int i0 = w; i0 < PIECES; i0 += 4 * CU_SIDE) {
+        uint4 c4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int it = min(i0 + i * CU_SIDE, PIECES - 1);
+          c4[i] = codes[it / PER * (2 * D) + it % PER * 32];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int it = i0 + i * CU_SIDE;
+          if (it < PIECES) work(it / PER, it % PER, c4[i]);
+        }
+      }
+    };
     // rows of the pass, 128 of them and zeros past the last one: [128 rows][64 dims] slabs, 16-byte chunk ch of row r at chunk ch ^ (r % 8) of its 128 bytes
     auto copy = [&](const void* base, long long row_stride, long long head_stride, uint8_t* to, int j0) {
       for (int x = ct; x < 128 * (D / 8); x += CT) {
@@ -282,12 +301,10 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           if (!go) break;
           if (cached) {
             const uint4* codes = reinterpret_cast<const uint4*>(code_s + (size_t)(C % CS) * 256 * D) + lane;
-#pragma unroll 4
-            for (int it = w; it < PIECES; it += CU_SIDE) {
-              const int p = it / PER, y = it % PER;
+            each_piece(codes, [&](int p, int y, const uint4& c4) {
               uint8_t* row = k_s + (D == 128 ? (y & 1) * 16384 + (y >> 1) * 1024 : y * 1024) + p * 2048 + x8 * 128;
-              widen(codes[p * (2 * D) + y * 32], row + c0, row + c1);
-            }
+              widen(c4, row + c0, row + c1);
+            });
           } else {
             copy(a.k, a.k_row, a.k_head, k_s, (tile - u.cached) * CU_NEW);
             cp_async_wait<0>();
@@ -312,13 +329,11 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
           if (!go) break;
           if (cached) {
             const uint4* codes = reinterpret_cast<const uint4*>(code_s + (size_t)(C % CS) * 256 * D) + D + lane;
-#pragma unroll 4
-            for (int it = w; it < PIECES; it += CU_SIDE) {
-              const int p = it / PER, y = it % PER;
+            each_piece(codes, [&](int p, int y, const uint4& c4) {
               uint8_t* row = v_s + (p >> 2) * (D * 128) + (y * 32 + lane) * 128;
               const uint32_t ch = (((p & 3) * 2) ^ x8) << 4;
-              widen(codes[p * (2 * D) + y * 32], row + ch, row + (ch ^ 16));
-            }
+              widen(c4, row + ch, row + (ch ^ 16));
+            });
           } else {
             copy(a.v, a.v_row, a.v_head, v_s, (tile - u.cached) * CU_NEW);
             cp_async_wait<0>();
