@@ -67,18 +67,17 @@ template <typename F> auto by_shape(const spec_cache* c, F f) {
 struct AttnShape {
   int mt;                       // (row, head) rows of a row tile: 16, 32 on mma.sync, 64, 128, 256 on tcgen05
   int limit;                    // (sequence, row tile) pairs of a launch
-  long long tiles, pairs;       // row tiles of a sequence; pairs of a launch at most
-  size_t arrive_bytes, bytes;
+  // Scratch: arrival counters of the mma.sync kernel, which are zero between calls and lie at the same place whatever the call's sizes; the tcgen05 kernel's notes for the joining kernel; parts.
+  size_t notes, parts, bytes;
 };
-AttnShape attn_shape(const spec_cache* c, int n_heads, int batch, int max_rows) {
+AttnShape attn_shape(const spec_cache* c, int n_heads, int max_rows) {
   AttnShape s;
   const long long rows = (long long)max_rows * (n_heads / c->n_kv_heads);
   s.mt = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   s.limit = s.mt <= 32 ? CAM_PAIRS : CU_PAIRS;
-  s.tiles = (rows + s.mt - 1) / s.mt;
-  s.pairs = s.tiles * batch < s.limit ? s.tiles * batch : s.limit;
-  s.arrive_bytes = ((size_t)s.pairs * c->n_kv_heads * 4 + 255) / 256 * 256;
-  s.bytes = s.arrive_bytes + (size_t)CAM_SMS * 2 * s.mt * (c->head_dim + 2) * 4;
+  s.notes = ((size_t)CAM_PAIRS * c->n_kv_heads * 4 + 255) / 256 * 256;
+  s.parts = s.notes + ((size_t)CU_PAIRS * c->n_kv_heads * 4 + 255) / 256 * 256;
+  s.bytes = s.parts + (size_t)CAM_SMS * 2 * s.mt * (c->head_dim + 2) * 4;
   return s;
 }
 template <typename K> int launch_attn(K kernel, int threads, size_t smem, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
@@ -86,13 +85,28 @@ template <typename K> int launch_attn(K kernel, int threads, size_t smem, const 
   kernel<<<CAM_SMS, threads, smem, st>>>(a, pl);
   return launched("spec_cache_attention");
 }
+// The tcgen05 kernel and, launched ahead of its end, the one that joins the parts of units that it cut.
+template <typename T, int D, int FMT, int ROWS> int launch_umma(const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
+  if (int rc = launch_attn(cache_attention_umma<T, D, FMT, ROWS>, CU_THREADS, cu_smem(D, ROWS), a, pl, st)) return rc;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(pl.nb * pl.nrt * a.c.kv, ROWS / CJ_ROWS);
+  cfg.blockDim = dim3(CJ_THREADS);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  cudaLaunchKernelEx(&cfg, cache_join_kernel<T, D, ROWS>, a, pl);
+  return launched("spec_cache_attention: join");
+}
 template <typename T, int D, int FMT> int launch_attn(int mt, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
   switch (mt) {
     case 16: return launch_attn(cache_attention_mma<T, D, FMT, 1>, CAM_THREADS, cam_smem(D), a, pl, st);
     case 32: return launch_attn(cache_attention_mma<T, D, FMT, 2>, CAM_THREADS, cam_smem(D), a, pl, st);
-    case 64: return launch_attn(cache_attention_umma<T, D, FMT, 64>, CU_THREADS, cu_smem(D, 64), a, pl, st);
-    case 128: return launch_attn(cache_attention_umma<T, D, FMT, 128>, CU_THREADS, cu_smem(D, 128), a, pl, st);
-    default: return launch_attn(cache_attention_umma<T, D, FMT, 256>, CU_THREADS, cu_smem(D, 256), a, pl, st);
+    case 64: return launch_umma<T, D, FMT, 64>(a, pl, st);
+    case 128: return launch_umma<T, D, FMT, 128>(a, pl, st);
+    default: return launch_umma<T, D, FMT, 256>(a, pl, st);
   }
 }
 unsigned copy_blocks(size_t units) {
@@ -236,7 +250,7 @@ int spec_cache_compact(const spec_cache* c, int32_t* used, void* scratch, size_t
 
 size_t spec_cache_attention_scratch(const spec_cache* c, int32_t n_heads, int32_t batch, int32_t max_rows) {
   if (cache_fault(c) || n_heads < 1 || n_heads % c->n_kv_heads || batch < 1 || max_rows < 1) return 0;
-  return attn_shape(c, n_heads, batch, max_rows).bytes;
+  return attn_shape(c, n_heads, max_rows).bytes;
 }
 
 int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void* scratch, size_t scratch_bytes, void* cuda_stream) {
@@ -253,7 +267,7 @@ int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void
       return fail(SPEC_E_BADARG, "spec_cache_attention: rows must start on 16-byte boundaries");
   }
   const int max_rows = r->max_rows < r->rows ? r->max_rows : r->rows;
-  const AttnShape sh = attn_shape(c, r->n_heads, r->batch, r->max_rows);
+  const AttnShape sh = attn_shape(c, r->n_heads, r->max_rows);
   if (!scratch || !aligned(scratch, 16) || scratch_bytes < sh.bytes) return fail(SPEC_E_NOMEM, "spec_cache_attention: scratch of %zu bytes, 16-byte aligned, is needed", sh.bytes);
   CacheAttnArgs a{view(c), r->q, r->k, r->v, r->q_row_stride, r->q_head_stride, r->k_row_stride, r->k_head_stride, r->v_row_stride, r->v_head_stride, r->out, r->lse, r->seqs, r->row_offsets,
                   r->mask, r->mask_words, r->rows, r->batch, r->n_heads, r->layer, max_rows, r->scale};
@@ -269,8 +283,8 @@ int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void
   const int nrt = tiles < sh.limit ? tiles : sh.limit, nb = sh.limit / nrt;
   for (int b0 = 0; b0 < r->batch; b0 += nb)
     for (int rt0 = 0; rt0 < tiles; rt0 += nrt) {
-      const CamPlan pl{b0, r->batch - b0 < nb ? r->batch - b0 : nb, rt0, tiles - rt0 < nrt ? tiles - rt0 : nrt, static_cast<int*>(scratch),
-                       reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + sh.arrive_bytes)};
+      uint8_t* room = static_cast<uint8_t*>(scratch);
+      const CamPlan pl{b0, r->batch - b0 < nb ? r->batch - b0 : nb, rt0, tiles - rt0 < nrt ? tiles - rt0 : nrt, reinterpret_cast<int*>(room + (sh.mt <= 32 ? 0 : sh.notes)), reinterpret_cast<float*>(room + sh.parts)};
       const int rc = by_shape(c, [&](auto d, auto f) {
         auto go = [&](auto t) {
           typedef decltype(t) T;

@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(16) uint64_t bars[20];
   __shared__ float2 consts[8][CAM_PAGES];                      // a page's scale of K with the score's factors, log2 of its scale of V; by cached tile
-  __shared__ int pre[CU_PAIRS + 1], scan[CU_WARPS], odd[8], last;
+  __shared__ int pre[CU_PAIRS + 1], scan[CU_WARPS], odd[8];
   __shared__ uint32_t tmem_slot;
   const uint32_t raw = smem_u32(smem_raw);
   uint8_t* q_s = smem_raw + (((raw + 1023u) & ~1023u) - raw);
@@ -94,6 +94,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   if (!list.template make<CU_THREADS>(pre, scan)) return;      // (all threads of the CTA agree, before anything is allocated)
   CamCursor u;
   if (!list.first(u)) return;
+  pdl_launch_dependents();                                     // (the joining kernel; it waits for this one's end)
   if (tid == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(code_full + i, 1);
@@ -673,19 +674,8 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       if (lane == 0) mbar_arrive(q_empty);
       tc_fence_before();
       if constexpr (ALT) softmax_bar();                         // (the accumulators may be written again)
-      if (!whole_unit) {
-        const int c0 = list.first_cta(u), c1 = list.last_cta(u);
-        __threadfence();
-        softmax_bar();
-        if (tid == 0) {
-          int* arrive = list.arrive(u);
-          last = atomicAdd(arrive, 1) == c1 - c0;
-          if (last) *arrive = 0;
-        }
-        softmax_bar();
-        if (last) cam_join<T, D, ROWS, CU_SOFT * 32>(list, u, rows, c0, c1, tid);
-        softmax_bar();                                          // (`last` may be written again)
-      }
+      // whose parts the joining kernel adds: written by the CTA that has the unit's first tile
+      if (tid == 0 && u.tile == 0) *list.arrive(u) = whole_unit ? 0 : (list.first_cta(u) + 1) << 16 | list.last_cta(u);
       C0 += max(0, min(u.tile1, u.cached) - u.tile);
       T0 += nt;
       ++U;
@@ -697,6 +687,57 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+}
+
+// Adds the parts of the units that were cut, in the order of their CTAs: a block 16 rows of a unit. In a kernel of its own all SMs take part; the last CTA of a unit alone took 8 us for five
+// parts of 64 rows, 25 for eighteen of 128.
+constexpr int CJ_THREADS = 128, CJ_ROWS = 16;
+template <typename T, int D, int MT>
+__global__ void __launch_bounds__(CJ_THREADS) cache_join_kernel(CacheAttnArgs a, CamPlan pl) {
+  pdl_wait();
+  const int unit = blockIdx.x, kvh = unit % a.c.kv, pair = unit / a.c.kv, b = pl.b0 + pair / pl.nrt, rtile = pl.rt0 + pair % pl.nrt, G = a.H / a.c.kv;
+  const int r0 = rows_begin(a.row_offsets, b, a.rows, a.batch), R = rows_begin(a.row_offsets, b + 1, a.rows, a.batch) - r0;
+  const int rows = min(MT, R * G - rtile * MT), first = blockIdx.y * CJ_ROWS;
+  if (first >= rows) return;
+  const int cut = pl.arrive[unit];
+  if (cut == 0) return;
+  const int c0 = (cut >> 16) - 1, c1 = cut & 0xffff;
+  constexpr int RP = CJ_THREADS / (D / 4), RB = CJ_ROWS / RP;
+  const int d = threadIdx.x % (D / 4) * 4, mine = first + threadIdx.x / (D / 4);
+  float top[RB], sum[RB];
+  float4 v[RB];
+#pragma unroll
+  for (int j = 0; j < RB; ++j) {
+    top[j] = -INFINITY;
+    sum[j] = 0.f;
+    v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+#pragma unroll 4
+  for (int k = c0; k <= c1; ++k) {
+    const float* in = pl.part + ((size_t)k * 2 + (k == c0 ? 1 : 0)) * ((size_t)MT * (D + 2));    // (the slots of CamList::part)
+    float2 e[RB];
+    float4 y[RB];
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+      const int r = min(mine + j * RP, rows - 1);
+      e[j] = __ldcg(reinterpret_cast<const float2*>(in + MT * D + 2 * r));
+      y[j] = __ldcg(reinterpret_cast<const float4*>(in + r * D + d));
+    }
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+      const float now = fmaxf(top[j], e[j].x), ref = now == -INFINITY ? 0.f : now;
+      const float f = ex2(top[j] - ref), h = ex2(e[j].x - ref);
+      sum[j] = f * sum[j] + h * e[j].y;
+      v[j].x = f * v[j].x + h * y[j].x;
+      v[j].y = f * v[j].y + h * y[j].y;
+      v[j].z = f * v[j].z + h * y[j].z;
+      v[j].w = f * v[j].w + h * y[j].w;
+      top[j] = now;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < RB; ++j)
+    if (mine + j * RP < rows) cam_finish<T, D, MT>(a, r0, rtile, kvh, mine + j * RP, d, top[j], sum[j], v[j]);
 }
 
 }  // namespace spec

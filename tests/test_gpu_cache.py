@@ -252,6 +252,22 @@ def test_attention_many_tiles_a_cta(torch, batch, heads, kv, D, n, rows, mask, f
     assert ((lse - wl).abs() <= 2.0 ** -14).all()
 
 
+def test_attention_calls_of_other_sizes_share_a_workspace(torch):
+    rng = np.random.default_rng(21)
+    c = _filled(rng, 1, 4, 128, [700, 90, 1500], "int8")
+    dev = _upload(torch, c)
+    sizes = [(1, 1), (3, 1), (1, 64), (3, 20), (1, 300), (3, 5), (2, 128), (3, 1), (1, 1)]
+    g = torch.Generator(device="cuda").manual_seed(5)
+    made = [[torch.randn((b * r, h, 128), generator=g, device="cuda").bfloat16() for h in (8, 4, 4)] for b, r in sizes]
+    alone = []
+    for (b, r), x in zip(sizes, made):
+        alone.append(_upload(torch, c).attention(0, *x, batch=b))
+    for _ in range(3):
+        for (b, r), x, want in zip(sizes, made, alone):
+            assert torch.equal(dev.attention(0, *x, batch=b), want), (b, r)
+    dev.check()
+
+
 def test_attention_long_cache_past_two_gigabytes(torch):
     # block offsets of more than 2^31 bytes: a pool of 2.3 GB of which the sequence holds the last pages
     from paper_2503_14153_b200 import SpecCache
