@@ -65,7 +65,7 @@ template <typename F> auto by_shape(const spec_cache* c, F f) {
 }
 
 struct AttnShape {
-  int mt;                       // (row, head) rows of a row tile: 16, 32 on mma.sync, 64, 128, 256 on tcgen05
+  int mt;                       // (row, head) rows of a row tile: 8, 16, 32 on mma.sync, 64, 128, 256 on tcgen05
   int limit;                    // (sequence, row tile) pairs of a launch
   // Scratch: arrival counters of the mma.sync kernel, which are zero between calls and lie at the same place whatever the call's sizes; the tcgen05 kernel's notes for the joining kernel; parts.
   size_t notes, parts, bytes;
@@ -73,16 +73,16 @@ struct AttnShape {
 AttnShape attn_shape(const spec_cache* c, int n_heads, int max_rows) {
   AttnShape s;
   const long long rows = (long long)max_rows * (n_heads / c->n_kv_heads);
-  s.mt = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  s.mt = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
   s.limit = s.mt <= 32 ? CAM_PAIRS : CU_PAIRS;
   s.notes = ((size_t)CAM_PAIRS * c->n_kv_heads * 4 + 255) / 256 * 256;
   s.parts = s.notes + ((size_t)CU_PAIRS * c->n_kv_heads * 4 + 255) / 256 * 256;
-  s.bytes = s.parts + (size_t)CAM_SMS * 2 * s.mt * (c->head_dim + 2) * 4;
+  s.bytes = s.parts + (size_t)(s.mt == 8 ? CAF_CTAS : CAM_SMS) * 2 * s.mt * (c->head_dim + 2) * 4;
   return s;
 }
-template <typename K> int launch_attn(K kernel, int threads, size_t smem, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
+template <typename K> int launch_attn(K kernel, int threads, size_t smem, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st, int ctas = CAM_SMS) {
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return launched("spec_cache_attention: shared memory");
-  kernel<<<CAM_SMS, threads, smem, st>>>(a, pl);
+  kernel<<<ctas, threads, smem, st>>>(a, pl);
   return launched("spec_cache_attention");
 }
 // The tcgen05 kernel and, launched ahead of its end, the one that joins the parts of units that it cut.
@@ -102,6 +102,7 @@ template <typename T, int D, int FMT, int ROWS> int launch_umma(const CacheAttnA
 }
 template <typename T, int D, int FMT> int launch_attn(int mt, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
   switch (mt) {
+    case 8: return launch_attn(cache_attention_few<T, D, FMT>, CAF_THREADS, (size_t)CAF_WARPS * CAF_ROWS * (D + 8) * 4, a, pl, st, CAF_CTAS);
     case 16: return launch_attn(cache_attention_mma<T, D, FMT, 1>, CAM_THREADS, cam_smem(D), a, pl, st);
     case 32: return launch_attn(cache_attention_mma<T, D, FMT, 2>, CAM_THREADS, cam_smem(D), a, pl, st);
     case 64: return launch_umma<T, D, FMT, 64>(a, pl, st);

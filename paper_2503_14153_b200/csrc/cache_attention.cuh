@@ -851,4 +851,300 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
   cp_async_wait<0>();
 }
 
+
+// ------------------------------------------------------------------ the kernel for at most eight rows
+// Single tokens with their group of query heads, and the smallest trees. The products are turned round: S^T = K Q^T and O^T = V^T P^T on m16n8k16, so that the 8-row side of the instruction has
+// the queries: half the instructions and half the accumulators of the 16-row form, which leaves room for 16 warps an SM. A warp takes a page at a time straight from global memory into the A operands'
+// registers (lane (g, t): 16 bytes of tokens g and g + 8, chunks t and t + 4, and the four tokens of place t of dims g, g + 8, ..), the next page on its way while one is worked on; nothing is staged. P^T
+// leaves S^T's registers by movmatrix. The reference is raised only when a weight passes cam_raise, so a page costs no reductions.
+// Bound by HBM from some thousand tokens a CTA on; below, by the chain lengths -> page numbers -> codes -> merge.
+constexpr int CAF_ROWS = 8, CAF_WARPS = 8, CAF_THREADS = 32 * CAF_WARPS, CAF_CTAS = 2 * CAM_SMS, CAF_UNIT = 2, CAF_NEW = 64;
+template <typename T> __host__ __device__ constexpr float cam_raise() { return std::is_same<T, bf16>::value ? 1.1529215046068470e18f : 4096.f; }   // 2^60; float16 weights stay below 2^16
+
+template <typename T, int D, int FMT>
+__global__ void __launch_bounds__(CAF_THREADS, 2) cache_attention_few(CacheAttnArgs a, CamPlan pl) {
+  constexpr int MT = CAF_ROWS, BLOCK = CACHE_PAGE * D, KC = D / 64, MTILES = D / 16, SR = D + 8;   // KC: chunks of 16 dims a lane has of a token; SR: floats of a row in shared memory
+  __shared__ int pre[CAM_PAIRS + 1];
+  __shared__ int scan[CAF_WARPS];
+  __shared__ int last;
+  __shared__ float2 sm[CAF_WARPS][MT];
+  extern __shared__ __align__(16) float so[];        // [CAF_WARPS][MT][SR]
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3, G = a.H / c.kv;
+  CamList<MT, CAF_NEW, CAF_UNIT> list{a, pl};
+  if (!list.template make<CAF_THREADS>(pre, scan)) return;
+  CamCursor u;
+  if (!list.first(u)) return;
+  const float scale2 = a.scale * 1.44269504088896f;
+
+  struct Page {
+    uint4 k[2][KC];                                  // tokens g, g + 8
+    uint32_t v[2 * MTILES];                          // dims 8 i + g
+  };
+  for (bool go = true; go; go = list.next(u)) {
+    const int R = u.R, n = u.n, r0 = u.r0, kvh = u.kvh, rtile = pl.rt0 + u.rt, rows = min(MT, R * G - rtile * MT);
+    const size_t head_block = ((size_t)a.layer * c.kv + kvh) * c.n_pages;
+    const int P0 = u.tile * CAM_PAGES, P1 = min((n + CACHE_PAGE - 1) / CACHE_PAGE, u.tile1 * CAM_PAGES);
+
+    // ---- q: row g's dims 16 t + 64 i .. + 15, as B operands; its factor goes to the lanes that have the row's scores
+    uint32_t qf[4 * KC][2];
+    float rs[2];
+    {
+      const int m = rtile * MT + g, qi = m / G;
+      const bool live = qi < R;
+      const T* qp = static_cast<const T*>(a.q) + (long long)(r0 + (live ? qi : 0)) * a.q_row + (long long)(kvh * G + (live ? m - qi * G : 0)) * a.q_head + 16 * t4;
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint4 w = live ? *reinterpret_cast<const uint4*>(qp + 64 * i + 8 * h) : make_uint4(0u, 0u, 0u, 0u);
+          qf[4 * i + 2 * h][0] = w.x;
+          qf[4 * i + 2 * h][1] = w.y;
+          qf[4 * i + 2 * h + 1][0] = w.z;
+          qf[4 * i + 2 * h + 1][1] = w.w;
+        }
+      float back = 1.f;
+      if constexpr (std::is_same<T, bf16>::value) {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * KC; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float2 v = unpack2<T>(qf[i][h]);
+            top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+          }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int ex = (int)(__float_as_uint(top) >> 23);                 // largest value into [2^8, 2^9)
+        const int up = ex == 0 || ex == 255 ? 0 : max(-120, min(120, 135 - ex));
+        const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+        back = __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+        for (int i = 0; i < 4 * KC; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float2 v = unpack2<T>(qf[i][h]);
+            qf[i][h] = pack2<f16>(v.x * f, v.y * f);
+          }
+      }
+      back *= scale2 * code_unit<FMT>();
+      rs[0] = __shfl_sync(0xffffffffu, back, 8 * t4);
+      rs[1] = __shfl_sync(0xffffffffu, back, 8 * t4 + 4);
+    }
+    float o[MTILES][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};     // rows 2 t, 2 t + 1: O^T of dims 16 i + g (0, 1) and 16 i + 8 + g (2, 3)
+#pragma unroll
+    for (int i = 0; i < MTILES; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    auto raise_to = [&](float top0, float top1) {
+      const float n0 = fmaxf(m[0], top0), n1 = fmaxf(m[1], top1);
+      const float f0 = n0 > m[0] ? ex2(m[0] - n0) : 1.f, f1 = n1 > m[1] ? ex2(m[1] - n1) : 1.f;
+      m[0] = n0;
+      m[1] = n1;
+      l[0] *= f0;
+      l[1] *= f1;
+#pragma unroll
+      for (int i = 0; i < MTILES; ++i) {
+        o[i][0] *= f0;
+        o[i][1] *= f1;
+        o[i][2] *= f0;
+        o[i][3] *= f1;
+      }
+    };
+    auto load = [&](Page& x, int page) {
+      const uint8_t* src = c.codes + (head_block + max(page, 0)) * (2 * (size_t)BLOCK);     // (a page that is not there: page 0's codes, with weight 0)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < KC; ++i) x.k[h][i] = __ldg(reinterpret_cast<const uint4*>(src + h * 8 * D + (t4 + 4 * i) * 128 + g * 16));
+#pragma unroll
+      for (int i = 0; i < 2 * MTILES; ++i) x.v[i] = __ldg(reinterpret_cast<const uint32_t*>(src + BLOCK + (8 * i + g) * 16 + t4 * 4));
+    };
+    auto work = [&](const Page& x, float ks, float lg, float inv, int keys) {               // keys: how many of the page's are there
+      float z[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < KC; ++i) {
+        const uint32_t w0[4] = {x.k[0][i].x, x.k[0][i].y, x.k[0][i].z, x.k[0][i].w}, w1[4] = {x.k[1][i].x, x.k[1][i].y, x.k[1][i].z, x.k[1][i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t f[4];
+          codes_to_f16<FMT>(w0[j], f[0], f[2]);
+          codes_to_f16<FMT>(w1[j], f[1], f[3]);
+          cam_mma<f16>(j & 1 ? y : z, f, qf[4 * i + j][0], qf[4 * i + j][1]);
+        }
+      }
+      const float f0 = rs[0] * ks, f1 = rs[1] * ks;
+      z[0] = (z[0] + y[0]) * f0 + lg;                // tokens g (0, 1) and g + 8 (2, 3), rows 2 t and 2 t + 1
+      z[1] = (z[1] + y[1]) * f1 + lg;
+      z[2] = (z[2] + y[2]) * f0 + lg;
+      z[3] = (z[3] + y[3]) * f1 + lg;
+      if (keys < CACHE_PAGE) {
+        if (g >= keys) z[0] = z[1] = -INFINITY;
+        if (g + 8 >= keys) z[2] = z[3] = -INFINITY;
+      }
+      float w[4];
+      auto weigh = [&]() {                           // (without a reference yet, a key weighs infinity; one that is not there, nothing)
+        w[0] = z[0] == -INFINITY ? 0.f : ex2(z[0] - m[0]);
+        w[1] = z[1] == -INFINITY ? 0.f : ex2(z[1] - m[1]);
+        w[2] = z[2] == -INFINITY ? 0.f : ex2(z[2] - m[0]);
+        w[3] = z[3] == -INFINITY ? 0.f : ex2(z[3] - m[1]);
+      };
+      weigh();
+      if (__any_sync(0xffffffffu, fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])) > cam_raise<T>())) {
+        float t0 = fmaxf(z[0], z[2]), t1 = fmaxf(z[1], z[3]);
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1) {
+          t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, s));
+          t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, s));
+        }
+        raise_to(t0, t1);
+        weigh();
+      }
+      l[0] += (w[0] + w[2]) * inv;
+      l[1] += (w[1] + w[3]) * inv;
+      uint32_t b0 = pack2<T>(w[0], w[1]), b1 = pack2<T>(w[2], w[3]);
+      asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(b0));
+      asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %0;" : "+r"(b1));
+#pragma unroll
+      for (int i = 0; i < MTILES; ++i) {
+        uint32_t f[4];
+        codes_to<FMT, T>(x.v[2 * i], f[0], f[2]);
+        codes_to<FMT, T>(x.v[2 * i + 1], f[1], f[3]);
+        cam_mma<T>(o[i], f, b0, b1);
+      }
+    };
+
+    // ---- cached pages: warp w takes P0 + w, + 8, ..; lane i knows number and scales of the i-th of 32
+    for (int base = P0 + warp; base < P1; base += 32 * CAF_WARPS) {
+      const int mine = base + CAF_WARPS * lane;
+      const int page = mine < P1 ? c.page(u.s, mine) : -1;
+      float2 sc = make_float2(0.f, 0.f);
+      Page x[2];
+      load(x[0], __shfl_sync(0xffffffffu, page, 0));
+      if (page >= 0) sc = *reinterpret_cast<const float2*>(c.scales + (head_block + page) * 2);
+      const float v = sc.y > 0.f ? sc.y * code_unit<FMT>() : 9.094947017729282e-13f;      // (a block of zeros: any factor would do; 2^-40 does not raise the reference)
+      const float lg = __log2f(v), inv = __fdividef(1.f, v);
+      const int count = min(32, (P1 - base + CAF_WARPS - 1) / CAF_WARPS);
+      for (int j = 0; j < count; j += 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (j + h >= count) break;
+          if (j + h + 1 < count) load(x[h ^ 1], __shfl_sync(0xffffffffu, page, j + h + 1));
+          const int keys = __shfl_sync(0xffffffffu, page, j + h) < 0 ? 0 : n - (base + CAF_WARPS * (j + h)) * CACHE_PAGE;
+          work(x[h], __shfl_sync(0xffffffffu, sc.x, j + h), __shfl_sync(0xffffffffu, lg, j + h), __shfl_sync(0xffffffffu, inv, j + h), keys);
+        }
+      }
+    }
+
+    // ---- rows of the pass, a warp a row at a time on CUDA cores: there are at most a few
+    if (u.tile1 > u.cached) {
+      for (int j = max(0, u.tile - u.cached) * CAF_NEW + warp; j < min(R, (u.tile1 - u.cached) * CAF_NEW); j += CAF_WARPS) {
+        constexpr int DL = D / 32;
+        const T* kp = static_cast<const T*>(a.k) + (long long)(r0 + j) * a.k_row + (long long)kvh * a.k_head + lane * DL;
+        float kd[DL], z[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < DL; ++e) kd[e] = to_f<T>(kp[e]);
+        bool see[2] = {false, false};
+        for (int r = 0; r < rows; ++r) {
+          const int mm = rtile * MT + r, i = mm / G;
+          const T* qp = static_cast<const T*>(a.q) + (long long)(r0 + i) * a.q_row + (long long)(kvh * G + mm - i * G) * a.q_head + lane * DL;
+          float s = 0.f;
+#pragma unroll
+          for (int e = 0; e < DL; ++e) s += to_f<T>(qp[e]) * kd[e];
+          s = warp_sum(s) * scale2;
+          if ((r >> 1) == t4) {
+            const bool vis = row_sees(a.mask, a.mask_words, r0 + i, i, j);
+            if (r & 1) { z[1] = s; see[1] = vis; } else { z[0] = s; see[0] = vis; }
+          }
+        }
+        float w[2];
+        auto weigh = [&]() {
+          w[0] = see[0] ? ex2(z[0] - m[0]) : 0.f;
+          w[1] = see[1] ? ex2(z[1] - m[1]) : 0.f;
+        };
+        weigh();
+        if (__any_sync(0xffffffffu, fmaxf(w[0], w[1]) > cam_raise<T>())) {
+          raise_to(see[0] ? z[0] : -INFINITY, see[1] ? z[1] : -INFINITY);
+          weigh();
+        }
+        if (g == 0) {
+          l[0] += w[0];
+          l[1] += w[1];
+        }
+        const T* vp = static_cast<const T*>(a.v) + (long long)(r0 + j) * a.v_row + (long long)kvh * a.v_head + g;
+#pragma unroll
+        for (int i = 0; i < MTILES; ++i) {
+          const float v0 = to_f<T>(vp[16 * i]), v1 = to_f<T>(vp[16 * i + 8]);
+          if (see[0]) {                              // (a masked value may be anything)
+            o[i][0] += w[0] * v0;
+            o[i][2] += w[0] * v1;
+          }
+          if (see[1]) {
+            o[i][1] += w[1] * v0;
+            o[i][3] += w[1] * v1;
+          }
+        }
+      }
+    }
+
+    // ---- the warps' sums
+#pragma unroll
+    for (int s = 4; s < 32; s <<= 1) {
+      l[0] += __shfl_xor_sync(0xffffffffu, l[0], s);
+      l[1] += __shfl_xor_sync(0xffffffffu, l[1], s);
+    }
+    __syncthreads();                                 // (the last unit's have been read)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = 2 * t4 + e;
+      if (g == 0) sm[warp][r] = make_float2(m[e], l[e]);
+      float* to = so + (warp * MT + r) * SR + g;
+#pragma unroll
+      for (int i = 0; i < MTILES; ++i) {
+        to[16 * i] = o[i][e];
+        to[16 * i + 8] = o[i][2 + e];
+      }
+    }
+    __syncthreads();
+    const bool whole = u.tile == 0 && u.tile1 == u.tiles;
+    for (int x = tid; x < rows * (D / 4); x += CAF_THREADS) {
+      const int r = x / (D / 4), d = x % (D / 4) * 4;
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < CAF_WARPS; ++k) top = fmaxf(top, sm[k][r].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float sum = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < CAF_WARPS; ++k) {
+        const float2 e = sm[k][r];
+        const float f = ex2(e.x - ref);
+        const float4 y = *reinterpret_cast<const float4*>(so + (k * MT + r) * SR + d);
+        sum += f * e.y;
+        v.x += f * y.x;
+        v.y += f * y.y;
+        v.z += f * y.z;
+        v.w += f * y.w;
+      }
+      if (whole) {
+        cam_finish<T, D, MT>(a, r0, rtile, kvh, r, d, top, sum, v);
+      } else {
+        float* out = list.part(u, D);
+        *reinterpret_cast<float4*>(out + r * D + d) = v;
+        if (d == 0) *reinterpret_cast<float2*>(out + MT * D + 2 * r) = make_float2(top, sum);
+      }
+    }
+    if (!whole) {
+      const int c0 = list.first_cta(u), c1 = list.last_cta(u);
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        int* arrive = list.arrive(u);
+        last = atomicAdd(arrive, 1) == c1 - c0;
+        if (last) *arrive = 0;
+      }
+      __syncthreads();
+      if (last) cam_join<T, D, MT, CAF_THREADS>(list, u, rows, c0, c1, tid);
+    }
+  }
+}
+
 }  // namespace spec
