@@ -855,10 +855,10 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
 // ------------------------------------------------------------------ the kernel for at most eight rows
 // Single tokens with their group of query heads, and the smallest trees. The products are turned round: S^T = K Q^T and O^T = V^T P^T on m16n8k16, so that the 8-row side of the instruction has
 // the queries: half the instructions and half the accumulators of the 16-row form, which leaves room for 16 warps an SM. A warp takes a page at a time straight from global memory into the A operands'
-// registers (lane (g, t): 16 bytes of tokens g and g + 8, chunks t and t + 4, and the four tokens of place t of dims g, g + 8, ..), the next page on its way while one is worked on; nothing is staged. P^T
+// registers (lane (g, t): 16 bytes of tokens g and g + 8, chunks t and t + 4, and the four tokens of place t of dims g, g + 8, ..), the next page's K on its way while one is worked on, the pages after it asked into L2; nothing is staged. P^T
 // leaves S^T's registers by movmatrix. The reference is raised only when a weight passes cam_raise, so a page costs no reductions.
 // Bound by HBM from some thousand tokens a CTA on; below, by the chain lengths -> page numbers -> codes -> merge.
-constexpr int CAF_ROWS = 8, CAF_WARPS = 8, CAF_THREADS = 32 * CAF_WARPS, CAF_CTAS = 2 * CAM_SMS, CAF_UNIT = 2, CAF_NEW = 64;
+constexpr int CAF_ROWS = 8, CAF_WARPS = 8, CAF_THREADS = 32 * CAF_WARPS, CAF_CTAS = 2 * CAM_SMS, CAF_UNIT = 2, CAF_NEW = 64, CAF_AHEAD = 4;
 template <typename T> __host__ __device__ constexpr float cam_raise() { return std::is_same<T, bf16>::value ? 1.1529215046068470e18f : 4096.f; }   // 2^60; float16 weights stay below 2^16
 
 template <typename T, int D, int FMT>
@@ -877,9 +877,8 @@ __global__ void __launch_bounds__(CAF_THREADS, 2) cache_attention_few(CacheAttnA
   if (!list.first(u)) return;
   const float scale2 = a.scale * 1.44269504088896f;
 
-  struct Page {
+  struct Keys {
     uint4 k[2][KC];                                  // tokens g, g + 8
-    uint32_t v[2 * MTILES];                          // dims 8 i + g
   };
   for (bool go = true; go; go = list.next(u)) {
     const int R = u.R, n = u.n, r0 = u.r0, kvh = u.kvh, rtile = pl.rt0 + u.rt, rows = min(MT, R * G - rtile * MT);
@@ -949,16 +948,17 @@ __global__ void __launch_bounds__(CAF_THREADS, 2) cache_attention_few(CacheAttnA
         o[i][3] *= f1;
       }
     };
-    auto load = [&](Page& x, int page) {
-      const uint8_t* src = c.codes + (head_block + max(page, 0)) * (2 * (size_t)BLOCK);     // (a page that is not there: page 0's codes, with weight 0)
+    auto block_of = [&](int page) { return c.codes + (head_block + max(page, 0)) * (2 * (size_t)BLOCK); };     // (a page that is not there: page 0's codes, with weight 0)
+    auto load = [&](Keys& x, const uint8_t* src) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < KC; ++i) x.k[h][i] = __ldg(reinterpret_cast<const uint4*>(src + h * 8 * D + (t4 + 4 * i) * 128 + g * 16));
-#pragma unroll
-      for (int i = 0; i < 2 * MTILES; ++i) x.v[i] = __ldg(reinterpret_cast<const uint32_t*>(src + BLOCK + (8 * i + g) * 16 + t4 * 4));
     };
-    auto work = [&](const Page& x, float ks, float lg, float inv, int keys) {               // keys: how many of the page's are there
+    auto work = [&](const Keys& x, const uint8_t* src, float ks, float lg, float inv, int keys) {               // keys: how many of the page's are there
+      uint32_t vw[2 * MTILES];                       // V's words: dims 8 i + g, used behind the scores
+#pragma unroll
+      for (int i = 0; i < 2 * MTILES; ++i) vw[i] = __ldg(reinterpret_cast<const uint32_t*>(src + BLOCK + (8 * i + g) * 16 + t4 * 4));
       float z[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < KC; ++i) {
@@ -1006,8 +1006,8 @@ __global__ void __launch_bounds__(CAF_THREADS, 2) cache_attention_few(CacheAttnA
 #pragma unroll
       for (int i = 0; i < MTILES; ++i) {
         uint32_t f[4];
-        codes_to<FMT, T>(x.v[2 * i], f[0], f[2]);
-        codes_to<FMT, T>(x.v[2 * i + 1], f[1], f[3]);
+        codes_to<FMT, T>(vw[2 * i], f[0], f[2]);
+        codes_to<FMT, T>(vw[2 * i + 1], f[1], f[3]);
         cam_mma<T>(o[i], f, b0, b1);
       }
     };
@@ -1016,20 +1016,33 @@ __global__ void __launch_bounds__(CAF_THREADS, 2) cache_attention_few(CacheAttnA
     for (int base = P0 + warp; base < P1; base += 32 * CAF_WARPS) {
       const int mine = base + CAF_WARPS * lane;
       const int page = mine < P1 ? c.page(u.s, mine) : -1;
+      const int count = min(32, (P1 - base + CAF_WARPS - 1) / CAF_WARPS);
       float2 sc = make_float2(0.f, 0.f);
-      Page x[2];
-      load(x[0], __shfl_sync(0xffffffffu, page, 0));
+      // a page of K and V is 32 lines of 128 bytes (D = 64: 16): the warp asks L2 for the page CAF_AHEAD places on with one instruction
+      auto ahead = [&](int j) {
+        const int p = __shfl_sync(0xffffffffu, page, min(j, 31));
+        if (j < count && p >= 0 && lane < 2 * BLOCK / 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(block_of(p) + lane * 128));
+      };
+#pragma unroll
+      for (int j = 1; j < CAF_AHEAD; ++j) ahead(j);
+      Keys x[2];
+      const uint8_t* src = block_of(__shfl_sync(0xffffffffu, page, 0));
+      load(x[0], src);
       if (page >= 0) sc = *reinterpret_cast<const float2*>(c.scales + (head_block + page) * 2);
       const float v = sc.y > 0.f ? sc.y * code_unit<FMT>() : 9.094947017729282e-13f;      // (a block of zeros: any factor would do; 2^-40 does not raise the reference)
       const float lg = __log2f(v), inv = __fdividef(1.f, v);
-      const int count = min(32, (P1 - base + CAF_WARPS - 1) / CAF_WARPS);
       for (int j = 0; j < count; j += 2) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (j + h >= count) break;
-          if (j + h + 1 < count) load(x[h ^ 1], __shfl_sync(0xffffffffu, page, j + h + 1));
+          ahead(j + h + CAF_AHEAD);
+          const uint8_t* here = src;
+          if (j + h + 1 < count) {
+            src = block_of(__shfl_sync(0xffffffffu, page, j + h + 1));
+            load(x[h ^ 1], src);
+          }
           const int keys = __shfl_sync(0xffffffffu, page, j + h) < 0 ? 0 : n - (base + CAF_WARPS * (j + h)) * CACHE_PAGE;
-          work(x[h], __shfl_sync(0xffffffffu, sc.x, j + h), __shfl_sync(0xffffffffu, lg, j + h), __shfl_sync(0xffffffffu, inv, j + h), keys);
+          work(x[h], here, __shfl_sync(0xffffffffu, sc.x, j + h), __shfl_sync(0xffffffffu, lg, j + h), __shfl_sync(0xffffffffu, inv, j + h), keys);
         }
       }
     }
