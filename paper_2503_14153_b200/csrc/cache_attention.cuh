@@ -855,7 +855,7 @@ __global__ void __launch_bounds__(CAM_THREADS, 1) cache_attention_mma(CacheAttnA
 // ------------------------------------------------------------------ the kernel for at most eight rows
 // Single tokens with their group of query heads, and the smallest trees. The products are turned round: S^T = K Q^T and O^T = V^T P^T on m16n8k16, so that the 8-row side of the instruction has
 // the queries: half the instructions and half the accumulators of the 16-row form, which leaves room for 16 warps an SM. A warp takes a page at a time straight from global memory into the A operands'
-// registers (lane (g, t): 16 bytes of tokens g and g + 8, chunks t and t + 4, and the four tokens of place t of dims g, g + 8, ..), the next page's K on its way while one is worked on, the pages after it asked into L2; nothing is staged. P^T
+// registers (lane (g, t): 16 bytes of tokens g and g + 8, chunks t and t + 4, and the four tokens of place t of dims g, g + 8, ..), with the pages after it asked into L2; nothing is staged. P^T
 // leaves S^T's registers by movmatrix. The reference is raised only when a weight passes cam_raise, so a page costs no reductions.
 // Bound by HBM from some thousand tokens a CTA on; below, by the chain lengths -> page numbers -> codes -> merge.
 constexpr int CAF_ROWS = 8, CAF_WARPS = 8, CAF_THREADS = 32 * CAF_WARPS, CAF_CTAS = 2 * CAM_SMS, CAF_UNIT = 2, CAF_NEW = 64, CAF_AHEAD = 4;
@@ -1025,25 +1025,17 @@ __global__ void __launch_bounds__(CAF_THREADS, 2) cache_attention_few(CacheAttnA
       };
 #pragma unroll
       for (int j = 1; j < CAF_AHEAD; ++j) ahead(j);
-      Keys x[2];
-      const uint8_t* src = block_of(__shfl_sync(0xffffffffu, page, 0));
-      load(x[0], src);
       if (page >= 0) sc = *reinterpret_cast<const float2*>(c.scales + (head_block + page) * 2);
       const float v = sc.y > 0.f ? sc.y * code_unit<FMT>() : 9.094947017729282e-13f;      // (a block of zeros: any factor would do; 2^-40 does not raise the reference)
       const float lg = __log2f(v), inv = __fdividef(1.f, v);
-      for (int j = 0; j < count; j += 2) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (j + h >= count) break;
-          ahead(j + h + CAF_AHEAD);
-          const uint8_t* here = src;
-          if (j + h + 1 < count) {
-            src = block_of(__shfl_sync(0xffffffffu, page, j + h + 1));
-            load(x[h ^ 1], src);
-          }
-          const int keys = __shfl_sync(0xffffffffu, page, j + h) < 0 ? 0 : n - (base + CAF_WARPS * (j + h)) * CACHE_PAGE;
-          work(x[h], here, __shfl_sync(0xffffffffu, sc.x, j + h), __shfl_sync(0xffffffffu, lg, j + h), __shfl_sync(0xffffffffu, inv, j + h), keys);
-        }
+#pragma unroll 1
+      for (int j = 0; j < count; ++j) {
+        ahead(j + CAF_AHEAD);
+        const int p = __shfl_sync(0xffffffffu, page, j);
+        const uint8_t* src = block_of(p);
+        Keys x;
+        load(x, src);
+        work(x, src, __shfl_sync(0xffffffffu, sc.x, j), __shfl_sync(0xffffffffu, lg, j), __shfl_sync(0xffffffffu, inv, j), p < 0 ? 0 : n - (base + CAF_WARPS * j) * CACHE_PAGE);
       }
     }
 
