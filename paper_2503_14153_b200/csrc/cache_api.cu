@@ -171,12 +171,18 @@ int spec_cache_store(const spec_cache* c, const spec_store_args* r, void* cuda_s
   if (!aligned(r->k, 16) || !aligned(r->v, 16) || r->k_row_stride % vec || r->k_head_stride % vec || r->k_layer_stride % vec || r->v_row_stride % vec || r->v_head_stride % vec || r->v_layer_stride % vec)
     return fail(SPEC_E_BADARG, "spec_cache_store: rows must start on 16-byte boundaries");
   StoreArgs a{view(c), r->k, r->v, r->k_layer_stride, r->k_row_stride, r->k_head_stride, r->v_layer_stride, r->v_row_stride, r->v_head_stride, r->seqs, r->row_offsets, r->counts, r->path,
-              r->rows, r->batch, r->layer0, r->max_count, (r->max_count + CACHE_PAGE - 2) / CACHE_PAGE + 1};
+              r->rows, r->batch, r->layer0, r->max_count, (r->max_count + CACHE_PAGE - 2) / CACHE_PAGE + 1, 1};
+  if ((long long)a.slots * r->batch * r->layers * c->n_kv_heads >= 148 * 32) a.each = STORE_EACH;
   if ((long long)a.slots * r->batch > 0x7fffffffLL || r->layers > 65535) return fail(SPEC_E_BADARG, "spec_cache_store: batch too large");
-  const dim3 grid(a.slots * r->batch, (2 * c->n_kv_heads + STORE_WARPS - 1) / STORE_WARPS, r->layers);
+  const dim3 grid(a.slots * r->batch, (2 * c->n_kv_heads + STORE_WARPS * a.each - 1) / (STORE_WARPS * a.each), r->layers);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   by_shape(c, [&](auto d, auto f) {
-    by_type(r->type, [&](auto t) { cache_store_kernel<decltype(t), decltype(d)::value, decltype(f)::value><<<grid, 32 * STORE_WARPS, 0, st>>>(a); });
+    by_type(r->type, [&](auto t) {
+      auto kernel = cache_store_kernel<decltype(t), decltype(d)::value, decltype(f)::value>;
+      const int smem = 2 * STORE_WARPS * (int)sizeof(StoreRoom<decltype(t), decltype(d)::value>);
+      if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      kernel<<<grid, 32 * STORE_WARPS, smem, st>>>(a);
+    });
   });
   return launched("spec_cache_store");
 }

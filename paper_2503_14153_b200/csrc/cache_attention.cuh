@@ -154,14 +154,9 @@ __host__ __device__ constexpr int cam_stage_bytes(int D) { return 256 * D + 128;
 // ring, then the key groups' sums: [KG][MT][D] values and (max, sum) pairs
 __host__ __device__ constexpr size_t cam_smem(int D) { return (size_t)CAM_STAGES * cam_stage_bytes(D) + (size_t)CAM_WARPS * 16 * (D + 2) * 4; }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

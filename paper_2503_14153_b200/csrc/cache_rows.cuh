@@ -1,6 +1,8 @@
 // Rows on their way into the 8-bit paged cache and out of it: rotary positions, quantised store, read-back. All three move
 // each value once and are bound by HBM.
 #pragma once
+#include <type_traits>
+
 #include "cache_common.cuh"
 
 namespace spec {
@@ -118,8 +120,8 @@ __global__ void rotary_table_kernel(float2* table, const double* __restrict__ fr
 }
 
 // ------------------------------------------------------------------ store
-// Rows path[b][0..count) of sequence b's rows of the pass (rows 0..count without a path) become tokens len - count .. len - 1. A warp owns the
-// K or the V block of one (layer, head, page): 16 rows in registers, the scale from their largest magnitude by a warp reduction, one write. A page
+// Rows path[b][0..count) of sequence b's rows of the pass (rows 0..count without a path) become tokens len - count .. len - 1. A warp has the
+// K or V blocks of STORE_EACH (layer, head, page) one after another: 16 rows in registers, the scale from their largest magnitude by a warp reduction, one write. A page
 // that held tokens before (the first one, where the sequence does not end at a page's end) keeps a scale at least as large, and its older codes are
 // rounded once more where the scale grew. Rows after the sequence's end are written as zeros.
 struct StoreArgs {
@@ -127,7 +129,7 @@ struct StoreArgs {
   const void *k, *v;                   // [layers][rows][kv][D]
   long long k_layer, k_row, k_head, v_layer, v_row, v_head;
   const int *seqs, *row_offsets, *counts, *path;
-  int rows, batch, layer0, path_len, slots;   // slots: pages a sequence's rows may touch
+  int rows, batch, layer0, path_len, slots, each;   // slots: pages a sequence's rows may touch; each: blocks a warp stores
 };
 
 __device__ __forceinline__ int rows_begin(const int* row_offsets, int b, int rows, int batch) {
@@ -136,16 +138,152 @@ __device__ __forceinline__ int rows_begin(const int* row_offsets, int b, int row
 }
 
 constexpr int STORE_WARPS = 4;
+// Blocks a warp stores, one after another, where there are warps enough for the chip without: what leads to them (length, count, page, path: four trips to memory one behind the other) is looked up once.
+constexpr int STORE_EACH = 8;
 
-// D / 32 16-byte chunks a lane and block (a block has 16 rows x D/16 chunks)
+// A warp's room in shared memory for a block that is stored: the 16 rows in their own type, a row padded by 16 bytes, and the block's older codes. Two of them, so that the next block's rows are on their way
+// (cp.async, no registers) while one is encoded.
+template <typename T, int D> struct StoreRoom {
+  static constexpr int ROW = D * (int)sizeof(T) + 16;
+  alignas(16) uint8_t rows[CACHE_PAGE * ROW];
+  alignas(16) uint8_t codes[CACHE_PAGE * D];
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// `mine`: in lane t < 16, the row of the pass that becomes token t of the page, or -1 (zeros)
+template <typename T, int D>
+__device__ __forceinline__ void store_fetch(StoreRoom<T, D>& room, const T* __restrict__ in, long long stride, int mine, bool held, const uint8_t* code, int lane) {
+  constexpr int N = 16 / (int)sizeof(T), CH = D / N;            // 16-byte chunks of a row
+#pragma unroll
+  for (int i = 0; i < CACHE_PAGE * CH / 32; ++i) {
+    const int x = lane + 32 * i, t = x / CH, ch = x % CH, r = __shfl_sync(0xffffffffu, mine, t);
+    cp_async16(smem_u32(room.rows + t * StoreRoom<T, D>::ROW + ch * 16), in + (long long)max(r, 0) * stride + ch * N, r >= 0 ? 16 : 0);
+  }
+  if (held)
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) cp_async16(smem_u32(room.codes + (lane + 32 * i) * 16), code + (lane + 32 * i) * 16, 16);
+  cp_async_commit();
+}
+
+// One block of K (WHICH 0) or V (1) out of shared memory; tokens before `held` were there before, with scale `was`. Of the block's 16-byte chunks a lane has D / 32: of K number lane + 32 i, 16 dims of a
+// token; of V dims 2 lane + 64 (i / 2) + i % 2, all tokens of a dim.
+template <typename T, int D, int FMT, int WHICH>
+__device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int held, float was, uint4* code, float* scale, int lane) {
+  constexpr int CH = D / 32, N = 16 / (int)sizeof(T), ROW = StoreRoom<T, D>::ROW;
+  // largest finite magnitude. 16-bit types: as integers, two at a time; only where that finds an infinity or NaN value by value
+  float top = 0.f;
+  bool clean = true;
+  if constexpr (sizeof(T) == 2) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < CACHE_PAGE * D / N / 32; ++i) {
+      const int x = lane + 32 * i;
+      const uint4 v = *reinterpret_cast<const uint4*>(room.rows + x / (D / N) * ROW + x % (D / N) * 16);
+      m = __vmaxu2(__vmaxu2(m, v.x & 0x7fff7fffu), __vmaxu2(v.y & 0x7fff7fffu, __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+    }
+    const uint32_t most = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+    clean = most < (std::is_same<T, bf16>::value ? 0x7f80u : 0x7c00u);
+    const unsigned short bits = (unsigned short)most;
+    top = to_f<T>(*reinterpret_cast<const T*>(&bits));
+  }
+  if (sizeof(T) == 4 || !clean) {
+    top = 0.f;
+    bool odd = false;
+#pragma unroll 1
+    for (int x = lane; x < CACHE_PAGE * D / N; x += 32) {
+      const Vec<T, N> v = *reinterpret_cast<const Vec<T, N>*>(room.rows + x / (D / N) * ROW + x % (D / N) * 16);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float m = fabsf(to_f<T>(v.x[e]));
+        odd = odd || !(m < INFINITY);
+        top = m < INFINITY ? fmaxf(top, m) : top;
+      }
+    }
+    top = warp_max(top);
+    clean = !__any_sync(0xffffffffu, odd);
+  }
+  const float now = fmaxf(was, top < CACHE_FLUSH ? 0.f : top / code_max<FMT>());
+  const float inv = now > 0.f ? 1.f / now : 0.f, again = now > 0.f ? was / now : 0.f;
+  auto encode = [&](const float (&x)[4]) {
+    if (clean) return encode4_inside<FMT>(x, inv);
+    const float f[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+    return encode4<FMT>(f);
+  };
+  // older codes in the new scale
+  auto renew = [&](uint32_t w) {
+    if (again == 1.f) return w;
+    float f[4];
+    decode4<FMT>(w, f);
+    return encode4_inside<FMT>(f, again);
+  };
+  const uint4* older = reinterpret_cast<const uint4*>(room.codes);
+  if constexpr (WHICH == 0) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int j = lane + 32 * i, t = (j / (D / 2)) * 8 + (j & 7), d = ((j >> 3) % (D / 16)) * 16;
+      uint32_t w[4];
+      if (t < held) {
+        const uint4 o = older[j];
+        w[0] = renew(o.x);
+        w[1] = renew(o.y);
+        w[2] = renew(o.z);
+        w[3] = renew(o.w);
+      } else {
+        T v[16];
+#pragma unroll
+        for (int y = 0; y < 16 / N; ++y) *reinterpret_cast<Vec<T, N>*>(v + y * N) = *reinterpret_cast<const Vec<T, N>*>(room.rows + t * ROW + d * sizeof(T) + y * 16);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float f[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = to_f<T>(v[4 * u + e]);
+          w[u] = encode(f);
+        }
+      }
+      code[j] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH; i += 2) {
+      const int j = 2 * lane + 32 * i;
+      uint32_t w[2][4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float f[2][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int pl = 4 * u + e, t = 2 * (pl >> 2) + 8 * ((pl >> 1) & 1) + (pl & 1);     // the token at this place (the inverse of cache_place)
+          const Vec<T, 2> v = *reinterpret_cast<const Vec<T, 2>*>(room.rows + t * ROW + j * sizeof(T));
+          f[0][e] = to_f<T>(v.x[0]);
+          f[1][e] = to_f<T>(v.x[1]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          w[h][u] = encode(f[h]);
+          if (held > 0) {
+            // tokens 2 u, 2 u + 1, 2 u + 8, 2 u + 9 are at these four places
+            const uint32_t keep = (2 * u < held ? 0xffu : 0u) | (2 * u + 1 < held ? 0xff00u : 0u) | (2 * u + 8 < held ? 0xff0000u : 0u) | (2 * u + 9 < held ? 0xff000000u : 0u);
+            w[h][u] = (w[h][u] & ~keep) | (renew(reinterpret_cast<const uint32_t*>(older + j + h)[u]) & keep);
+          }
+        }
+      }
+      code[j] = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
+      code[j + 1] = make_uint4(w[1][0], w[1][1], w[1][2], w[1][3]);
+    }
+  }
+  if (lane == 0) *scale = now;
+}
+
 template <typename T, int D, int FMT>
 __global__ void __launch_bounds__(32 * STORE_WARPS) cache_store_kernel(StoreArgs a) {
-  constexpr int CH = D / 32;
+  extern __shared__ __align__(16) uint8_t store_smem[];
   const CacheView& c = a.c;
-  const int b = blockIdx.x / a.slots, slot = blockIdx.x % a.slots, lane = threadIdx.x & 31;
-  const int unit = blockIdx.y * STORE_WARPS + (threadIdx.x >> 5);
-  if (unit >= 2 * c.kv) return;
-  const int head = unit >> 1, which = unit & 1, layer = blockIdx.z;
+  const int b = blockIdx.x / a.slots, slot = blockIdx.x % a.slots, lane = threadIdx.x & 31, layer = blockIdx.z;
   const int s = c.sequence(a.seqs, b);
   if (s < 0) return;
   const int len = c.len(s), count = max(0, min(a.counts[b], len)), first = len - count;
@@ -155,7 +293,6 @@ __global__ void __launch_bounds__(32 * STORE_WARPS) cache_store_kernel(StoreArgs
   if (page < 0) return;
   const int base = p * CACHE_PAGE;     // token of the page's first row
   const int r0 = rows_begin(a.row_offsets, b, a.rows, a.batch), r1 = rows_begin(a.row_offsets, b + 1, a.rows, a.batch);
-  // the row of the pass that becomes row t of the page: -1 not a new one
   int mine = -1;
   if (lane < CACHE_PAGE && base + lane >= first && base + lane < len) {
     const int i = base + lane - first;
@@ -163,83 +300,34 @@ __global__ void __launch_bounds__(32 * STORE_WARPS) cache_store_kernel(StoreArgs
     if (r >= r0 && r < r1) mine = r;
     else set_status(c.status, ST_BOUNDS, 203, i);
   }
-  const size_t blk = c.block(a.layer0 + layer, head, page, which);
-  uint4* code = reinterpret_cast<uint4*>(c.codes + blk * (CACHE_PAGE * D));
-  const bool held = base < first;
-  const float was = held ? c.scales[blk] : 0.f;
-  float x[CH][16];                     // chunk i of the lane: number lane + 32 i (K) or the dims 2 lane + 64 (i / 2) + i % 2 (V)
-  float top = 0.f;
-  const T* in = static_cast<const T*>(which ? a.v : a.k) + layer * (which ? a.v_layer : a.k_layer) + head * (which ? a.v_head : a.k_head);
-  const long long rs = which ? a.v_row : a.k_row;
-  auto chunk_number = [&](int i) { return which ? 2 * lane + 64 * (i >> 1) + (i & 1) : lane + 32 * i; };
-  if (which == 0) {
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int j = lane + 32 * i, t = (j / (D / 2)) * 8 + (j & 7), d = ((j >> 3) % (D / 16)) * 16;
-      const int r = __shfl_sync(0xffffffffu, mine, t);
-      if (r >= 0) {
-        constexpr int N = 16 / sizeof(T);
-#pragma unroll
-        for (int u = 0; u < 16 / N; ++u) {
-          const Vec<T, N> w = *reinterpret_cast<const Vec<T, N>*>(in + r * rs + d + u * N);
-#pragma unroll
-          for (int e = 0; e < N; ++e) x[i][u * N + e] = to_f<T>(w.x[e]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[i][e] = 0.f;
-      }
+  const int each = STORE_WARPS * a.each, warp = threadIdx.x >> 5, held = max(0, first - base), end = min(2 * c.kv, ((int)blockIdx.y + 1) * each);
+  StoreRoom<T, D>* room = reinterpret_cast<StoreRoom<T, D>*>(store_smem) + 2 * warp;
+  auto block_of = [&](int unit) { return c.block(a.layer0 + layer, unit >> 1, page, unit & 1); };
+  float was[2] = {0.f, 0.f};
+  auto fetch = [&](int unit, int to) {
+    const T* in = unit & 1 ? static_cast<const T*>(a.v) + layer * a.v_layer + (unit >> 1) * a.v_head : static_cast<const T*>(a.k) + layer * a.k_layer + (unit >> 1) * a.k_head;
+    const size_t blk = block_of(unit);
+    was[to] = held > 0 ? c.scales[blk] : 0.f;
+    store_fetch<T, D>(room[to], in, unit & 1 ? a.v_row : a.k_row, mine, held > 0, c.codes + blk * (CACHE_PAGE * D), lane);
+  };
+  int unit = blockIdx.y * each + warp, at = 0;
+  if (unit < end) fetch(unit, 0);
+#pragma unroll 1
+  for (; unit < end; unit += STORE_WARPS, at ^= 1) {
+    if (unit + STORE_WARPS < end) {
+      at ? fetch(unit + STORE_WARPS, 0) : fetch(unit + STORE_WARPS, 1);
+      cp_async_wait<1>();
+    } else {
+      cp_async_wait<0>();
     }
-  } else {
-#pragma unroll
-    for (int t = 0; t < CACHE_PAGE; ++t) {
-      const int r = __shfl_sync(0xffffffffu, mine, t);
-#pragma unroll
-      for (int i = 0; i < CH; i += 2) {
-        Vec<T, 2> w{};
-        if (r >= 0) w = *reinterpret_cast<const Vec<T, 2>*>(in + r * rs + 2 * lane + 32 * i);
-        x[i][cache_place(t)] = r >= 0 ? to_f<T>(w.x[0]) : 0.f;
-        x[i + 1][cache_place(t)] = r >= 0 ? to_f<T>(w.x[1]) : 0.f;
-      }
-    }
+    __syncwarp();
+    const size_t blk = block_of(unit);
+    uint4* code = reinterpret_cast<uint4*>(c.codes + blk * (CACHE_PAGE * D));
+    const float w = at ? was[1] : was[0];
+    if (unit & 1) store_block<T, D, FMT, 1>(room[at], held, w, code, c.scales + blk, lane);
+    else store_block<T, D, FMT, 0>(room[at], held, w, code, c.scales + blk, lane);
+    __syncwarp();                        // (the room is fetched into again)
   }
-#pragma unroll
-  for (int i = 0; i < CH; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float m = fabsf(x[i][e]);
-      top = m < INFINITY ? fmaxf(top, m) : top;          // (neither infinities nor NaN count for the scale)
-    }
-  top = warp_max(top);
-  const float now = fmaxf(was, top < CACHE_FLUSH ? 0.f : top / code_max<FMT>());
-  const float inv = now > 0.f ? 1.f / now : 0.f, again = now > 0.f ? was / now : 0.f;
-#pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    const int j = chunk_number(i);
-    uint4 old = make_uint4(0, 0, 0, 0);
-    if (held) old = code[j];
-    uint32_t w[4];
-    const uint32_t o4[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      float f[4], g[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f[e] = x[i][4 * u + e] * inv;
-      if (held) {
-        decode4<FMT>(o4[u], g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          // token of this value: of the chunk (K), or by its place (V: the inverse of cache_place)
-          const int pl = 4 * u + e;
-          const int t = which ? 2 * (pl >> 2) + 8 * ((pl >> 1) & 1) + (pl & 1) : (j / (D / 2)) * 8 + (j & 7);
-          if (base + t < first) f[e] = g[e] * again;
-        }
-      }
-      w[u] = encode4<FMT>(f);
-    }
-    code[j] = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-  if (lane == 0) c.scales[blk] = now;
 }
 
 // ------------------------------------------------------------------ read
