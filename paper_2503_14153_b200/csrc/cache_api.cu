@@ -136,14 +136,17 @@ int spec_rotary(const spec_rotary_args* r, void* cuda_stream) {
   if (!known_type(r->in_type) || !known_type(r->out_type)) return fail(SPEC_E_BADARG, "spec_rotary: unknown type");
   RotaryArgs a{r->q, r->k, r->v, r->q_row_stride, r->k_row_stride, r->v_row_stride, r->q_head_stride, r->k_head_stride, r->v_head_stride, r->q_out, r->k_out, r->v_out,
                r->positions, reinterpret_cast<const float2*>(r->table), r->rows, r->n_heads, r->n_kv_heads, r->n_v_heads, r->head_dim, r->rot_dim, r->span};
-  // four pairs a thread where every access of four elements is aligned
-  const size_t vi = 4 * elem_size(r->in_type), vo = 4 * elem_size(r->out_type);
-  const bool strides = r->q_row_stride % 4 == 0 && r->q_head_stride % 4 == 0 && r->k_row_stride % 4 == 0 && r->k_head_stride % 4 == 0 && r->v_row_stride % 4 == 0 && r->v_head_stride % 4 == 0;
-  const bool wide = r->head_dim % 8 == 0 && r->rot_dim % 8 == 0 && strides && aligned(r->q, vi) && aligned(r->k, vi) && aligned(r->v, vi) && aligned(r->q_out, vo) && aligned(r->k_out, vo) && aligned(r->v_out, vo);
-  const int per_head = r->rot_dim / 2 / (wide ? 4 : 1), sweep = ROT_THREADS / per_head > 0 ? ROT_THREADS / per_head : 1;
+  // 16-byte reads (8 pairs a thread of 16-bit inputs, 4 of 32-bit ones) where every access is aligned, else 4 pairs, else one
+  auto fits = [&](int v) {
+    const size_t vi = (size_t)v * elem_size(r->in_type), vo = (size_t)v * elem_size(r->out_type) > 16 ? 16 : (size_t)v * elem_size(r->out_type);
+    const bool strides = r->q_row_stride % v == 0 && r->q_head_stride % v == 0 && r->k_row_stride % v == 0 && r->k_head_stride % v == 0 && r->v_row_stride % v == 0 && r->v_head_stride % v == 0;
+    return r->head_dim % (2 * v) == 0 && r->rot_dim % (2 * v) == 0 && strides && aligned(r->q, vi) && aligned(r->k, vi) && aligned(r->v, vi) && aligned(r->q_out, vo) && aligned(r->k_out, vo) && aligned(r->v_out, vo);
+  };
+  const int width = r->in_type != SPEC_TYPE_F32 && fits(8) ? 8 : fits(4) ? 4 : 1;
+  const int per_head = r->rot_dim / 2 / width, sweep = ROT_THREADS / per_head > 0 ? ROT_THREADS / per_head : 1;
   const int heads = r->n_heads + r->n_kv_heads;
-  // parts of the heads so that a few rows, too, fill the SMs; a block keeps ROT_HEADS sweeps where there are rows enough
-  int parts = (heads + sweep * ROT_HEADS - 1) / (sweep * ROT_HEADS);
+  // parts of the heads so that a few rows, too, fill the SMs; a block keeps rot_heads sweeps where there are rows enough
+  int parts = (heads + sweep * rot_heads(width) - 1) / (sweep * rot_heads(width));
   while (parts * sweep < heads && (long long)parts * r->rows < 148 * 8) ++parts;
   if (parts < 1) parts = 1;
   const dim3 grid(r->rows, parts < 65535 ? parts : 65535);
@@ -152,8 +155,13 @@ int spec_rotary(const spec_rotary_args* r, void* cuda_stream) {
     by_type(r->out_type, [&](auto to) {
       typedef decltype(ti) TI;
       typedef decltype(to) TO;
-      if (wide) r->interleaved ? rotary_kernel<TI, TO, true, 4><<<grid, ROT_THREADS, 0, st>>>(a) : rotary_kernel<TI, TO, false, 4><<<grid, ROT_THREADS, 0, st>>>(a);
-      else r->interleaved ? rotary_kernel<TI, TO, true, 1><<<grid, ROT_THREADS, 0, st>>>(a) : rotary_kernel<TI, TO, false, 1><<<grid, ROT_THREADS, 0, st>>>(a);
+      auto go = [&](auto v) {
+        constexpr int V = decltype(v)::value;
+        r->interleaved ? rotary_kernel<TI, TO, true, V><<<grid, ROT_THREADS, 0, st>>>(a) : rotary_kernel<TI, TO, false, V><<<grid, ROT_THREADS, 0, st>>>(a);
+      };
+      if constexpr (sizeof(TI) == 2)
+        if (width == 8) return go(Int<8>{});
+      width == 4 ? go(Int<4>{}) : go(Int<1>{});
     });
   });
   return launched("spec_rotary");

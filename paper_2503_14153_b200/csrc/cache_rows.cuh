@@ -11,7 +11,7 @@ namespace spec {
 // Pair i of a head, (x1, x2) = (x[i], x[i + rot/2]) in the half layout, (x[2i], x[2i+1]) in the interleaved one, turns by the table's
 // angle of the row's position: y1 = x1 c - x2 s, y2 = x2 c + x1 s. Dims from `rot` on, and all of v, are only cast.
 constexpr int ROT_THREADS = 128;
-constexpr int ROT_HEADS = 4;    // heads whose loads a thread has in flight
+__host__ __device__ constexpr int rot_heads(int V) { return V == 8 ? 2 : 4; }    // heads whose loads a thread has in flight
 
 struct RotaryArgs {
   const void *q, *k, *v;
@@ -22,12 +22,13 @@ struct RotaryArgs {
   int rows, H, kv, kvv, D, rot, span;    // kvv: heads of v (0: none)
 };
 
-template <typename T, int N> struct alignas(sizeof(T) * N) Vec { T x[N]; };
+template <typename T, int N> struct alignas(sizeof(T) * N > 16 ? 16 : sizeof(T) * N) Vec { T x[N]; };
 
-// V pairs a thread: V = 4 where pointers, strides and rot allow 4-element accesses, else 1. A thread keeps its (cos, sin) in registers and
+// V pairs a thread: 8 (16-bit inputs) or 4 where pointers, strides and rot allow accesses of so many elements, else 1. A thread keeps its (cos, sin) in registers and
 // goes over the heads, ROT_HEADS at a time in flight. blockIdx = (row, part of the heads).
 template <typename TI, typename TO, bool IL, int V>
 __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
+  constexpr int HU = rot_heads(V);
   const int row = blockIdx.x;
   const int pos = a.positions[row];
   const bool inside = pos >= 0 && pos < a.span;     // (a row whose position the table does not hold becomes NaN)
@@ -52,10 +53,10 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
       s[j] = cs.y;
     }
     const int step = lane_heads * gridDim.y;
-    for (int h0 = blockIdx.y * lane_heads + hs; h0 < heads; h0 += step * ROT_HEADS) {
-      Vec<TI, V> lo[ROT_HEADS], hi[ROT_HEADS];
+    for (int h0 = blockIdx.y * lane_heads + hs; h0 < heads; h0 += step * HU) {
+      Vec<TI, V> lo[HU], hi[HU];
 #pragma unroll
-      for (int u = 0; u < ROT_HEADS; ++u) {
+      for (int u = 0; u < HU; ++u) {
         const int h = h0 + u * step;
         if (h >= heads) break;
         const TI* p = src(h) + (IL ? 2 * V * g : V * g);
@@ -63,7 +64,7 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(RotaryArgs a) {
         hi[u] = *reinterpret_cast<const Vec<TI, V>*>(p + (IL ? V : half));
       }
 #pragma unroll
-      for (int u = 0; u < ROT_HEADS; ++u) {
+      for (int u = 0; u < HU; ++u) {
         const int h = h0 + u * step;
         if (h >= heads) break;
         Vec<TO, V> yl, yh;
