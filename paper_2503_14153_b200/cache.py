@@ -14,6 +14,7 @@ A step of a program that runs the layers itself:
 import ctypes as C
 import functools
 import math
+import struct
 from typing import Optional, Tuple
 
 from .binding import SpecError, _torch, load_library
@@ -47,6 +48,17 @@ class _RotaryArgs(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v", "q_out", "k_out", "v_out", "positions", "table")] + \
                [(n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head")] + \
                [(n, C.c_int32) for n in ("in_type", "out_type", "rows", "n_heads", "n_kv_heads", "n_v_heads", "head_dim", "rot_dim", "span", "interleaved")]
+
+
+_CODE = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f"}
+
+
+def _packer(cls):
+    """The structure's bytes from its fields in order: a third of the time that filling a ctypes structure takes."""
+    return struct.Struct("".join(_CODE[t] for _, t in cls._fields_)).pack
+
+
+_pack_attention, _pack_store, _pack_read, _pack_rotary = _packer(_AttentionArgs), _packer(_StoreArgs), _packer(_ReadArgs), _packer(_RotaryArgs)
 
 
 @functools.lru_cache(maxsize=1)
@@ -111,6 +123,7 @@ class SpecCache:
         self._p = C.addressof(self._c)
         self.lib, self._torch, self._raw_stream, self._types = _library()
         self._index = self.device.index
+        self._scale = 1.0 / math.sqrt(D) if D else 0.0
         self._work = {}                          # workspaces by (stream, kind): calls on different streams may overlap
         self._sizes = {}
         if not self.lib.spec_cache_scratch_bytes(self._p):
@@ -127,7 +140,7 @@ class SpecCache:
     def _ints(self, t, n: Optional[int], what: str):
         """Address of an int32 vector on the cache's device (None: 0)."""
         if t is None:
-            return None
+            return 0
         if t.dtype != self._torch.int32 or t.device != self.device or not t.is_contiguous() or (n is not None and t.numel() != n):
             _bad(f"{what}: expected a contiguous int32 tensor{'' if n is None else f' of {n} values'} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         return t.data_ptr()
@@ -151,42 +164,49 @@ class SpecCache:
         q [rows, heads, D], k and v [rows, kv heads, D] (bf16, f16 or f32, all alike; any row and head strides that keep rows on 16-byte boundaries). `batch` groups of rows
         / batch rows each, or given by row_offsets (int32 [batch + 1] on the device; then max_rows bounds the rows of a group). seqs: the groups' sequences (0 .. batch - 1).
         mask: int32 [rows, words], bit j of a row: it sees row j of its group; None: causal. Returns out, or (out, lse) with lse=True."""
-        lib, torch = self.lib, self._torch
-        rows, heads = q.shape[0], q.shape[1]
-        self._rows(q, None, "attention: q")
-        self._rows(k, self.n_kv_heads, "attention: k")
-        self._rows(v, self.n_kv_heads, "attention: v")
-        if not q.dtype == k.dtype == v.dtype or k.shape[0] != rows or v.shape[0] != rows:
-            _bad("attention: q, k and v must have the same rows and type")
+        lib, torch, device, D, dtype = self.lib, self._torch, self.device, self.head_dim, q.dtype
+        kind = self._types.get(dtype)
+        if kind is None or q.dim() != 3:
+            _bad("attention: q must be [rows, heads, D] of bfloat16, float16 or float32")
+        rows, heads, width = q.shape
+        kv_shape, (q0, q1, q2), (k0, k1, k2), (v0, v1, v2) = (rows, self.n_kv_heads, D), q.stride(), self._stride3(k, "k"), self._stride3(v, "v")
+        if width != D or k.shape != kv_shape or v.shape != kv_shape or k.dtype != dtype or v.dtype != dtype or q2 != 1 or k2 != 1 or v2 != 1 or q.device != device or k.device != device or v.device != device:
+            _bad(f"attention: expected q [rows, heads, {D}], k and v {list(kv_shape)}, one type, contiguous last dimension, on {device}; got {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}, "
+                 f"{q.dtype}, {k.dtype}, {v.dtype} on {q.device}, {k.device}, {v.device}")
         if row_offsets is None:
             if batch < 1 or rows % batch:
                 _bad(f"attention: {rows} rows do not divide among {batch} groups")
-            max_rows = max(1, rows // batch)
+            max_rows = rows // batch or 1
         elif max_rows is None:
             _bad("attention: row_offsets needs max_rows")
-        words = 0
+        words = mask_at = 0
         if mask is not None:
-            if mask.dim() != 2 or mask.shape[0] != rows or mask.dtype != torch.int32 or mask.device != self.device or not mask.is_contiguous():
+            if mask.dim() != 2 or mask.shape[0] != rows or mask.dtype != torch.int32 or mask.device != device or not mask.is_contiguous():
                 _bad("attention: mask must be a contiguous int32 tensor [rows, words] on the cache's device")
-            words = mask.shape[1]
+            words, mask_at = mask.shape[1], mask.data_ptr()
         if out is None:
-            out = torch.empty((rows, heads, self.head_dim), dtype=q.dtype, device=self.device)
-        elif out.dtype != q.dtype or out.shape != q.shape or not out.is_contiguous() or out.device != self.device:
+            out = torch.empty((rows, heads, D), dtype=dtype, device=device)
+        elif out.dtype != dtype or out.shape != q.shape or not out.is_contiguous() or out.device != device:
             _bad("attention: out must be contiguous, of q's shape and type")
-        sums = torch.empty((rows, heads), dtype=torch.float32, device=self.device) if lse else None
-        qs, ks, vs = q.stride(), k.stride(), v.stride()
-        a = _AttentionArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), sums.data_ptr() if lse else None, self._ints(seqs, batch, "attention: seqs"),
-                           self._ints(row_offsets, batch + 1, "attention: row_offsets"), mask.data_ptr() if words else None, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1],
-                           self._types[q.dtype], rows, batch, heads, layer, max_rows, words, 1.0 / math.sqrt(self.head_dim) if scale is None else scale)
-        key = (heads, batch, max_rows)
+        sums = torch.empty((rows, heads), dtype=torch.float32, device=device) if lse else None
+        a = _pack_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), sums.data_ptr() if lse else 0, self._ints(seqs, batch, "attention: seqs"),
+                            self._ints(row_offsets, batch + 1, "attention: row_offsets"), mask_at, q0, q1, k0, k1, v0, v1, kind, rows, batch, heads, layer, max_rows, words,
+                            self._scale if scale is None else scale)
+        key = heads, max_rows
         need = self._sizes.get(key)
         if need is None:
             need = self._sizes[key] = lib.spec_cache_attention_scratch(self._p, heads, batch, max_rows)
         stream = self._raw_stream(self._index)
-        rc = lib.spec_cache_attention(self._p, C.addressof(a), self._workspace(stream, "attention", need), need, stream)
+        rc = lib.spec_cache_attention(self._p, a, self._workspace(stream, "attention", need), need, stream)
         if rc:
             _raise(rc)
         return (out, sums) if lse else out
+
+    @staticmethod
+    def _stride3(t, what):
+        if t.dim() != 3:
+            _bad(f"attention: {what} must be [rows, kv heads, D]")
+        return t.stride()
 
     def store(self, k, v, counts, *, batch: Optional[int] = None, row_offsets=None, seqs=None, path=None, max_count: Optional[int] = None, layer0: int = 0):
         """Rows k, v [layers, rows, kv heads, D] of a pass into the cache: the rows path[b][:counts[b]] of group b (its first counts[b] without a path) become the last counts[b] tokens of
@@ -209,9 +229,9 @@ class SpecCache:
         if row_offsets is None and batch and rows % batch:
             _bad(f"store: {rows} rows do not divide among {batch} groups")
         ks, vs = k.stride(), v.stride()
-        a = _StoreArgs(k.data_ptr(), v.data_ptr(), self._ints(seqs, batch, "store: seqs"), self._ints(row_offsets, batch + 1, "store: row_offsets"), self._ints(counts, batch, "store: counts"),
+        a = _pack_store(k.data_ptr(), v.data_ptr(), self._ints(seqs, batch, "store: seqs"), self._ints(row_offsets, batch + 1, "store: row_offsets"), self._ints(counts, batch, "store: counts"),
                        self._ints(path, None, "store: path"), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], self._types[k.dtype], rows, batch, layer0, layers, max_count)
-        rc = self.lib.spec_cache_store(self._p, C.addressof(a), self._raw_stream(self._index))
+        rc = self.lib.spec_cache_store(self._p, a, self._raw_stream(self._index))
         if rc:
             _raise(rc)
 
@@ -224,8 +244,8 @@ class SpecCache:
         if dtype not in self._types:
             _bad("read: dtype must be bfloat16, float16 or float32")
         k, v = (torch.empty((max(layers, 0), batch, max(window, 0), self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device) for _ in "kv")
-        a = _ReadArgs(k.data_ptr(), v.data_ptr(), self._ints(seqs, batch, "read: seqs"), self._ints(start, batch, "read: start"), self._types[dtype], batch, window, layer0, layers)
-        rc = self.lib.spec_cache_read(self._p, C.addressof(a), self._raw_stream(self._index))
+        a = _pack_read(k.data_ptr(), v.data_ptr(), self._ints(seqs, batch, "read: seqs"), self._ints(start, batch, "read: start"), self._types[dtype], batch, window, layer0, layers)
+        rc = self.lib.spec_cache_read(self._p, a, self._raw_stream(self._index))
         if rc:
             _raise(rc)
         return k, v
@@ -276,25 +296,30 @@ def spec_rotary(q, k, v, positions, table, *, interleaved: bool = False, dtype=N
     """Rotated q and k, and v cast, all contiguous in `dtype` (default: q's). q [rows, heads, D], k and v [rows, kv heads, D] may be strided views of one projection's output (v may
     be None); positions int32 [rows]; table float32 [span, rot / 2, 2] from spec_rotary_table: the first `rot` dims of every head of q and k turn."""
     lib, torch, raw_stream, types = _library()
-    rows, D = q.shape[0], q.shape[-1]
-    dtype = q.dtype if dtype is None else dtype
-    for t, what in ((q, "q"), (k, "k"), (v, "v")):
-        if t is not None and (t.dim() != 3 or t.shape[0] != rows or t.shape[2] != D or t.dtype != q.dtype or t.stride(2) != 1 or t.device != q.device):
-            _bad(f"spec_rotary: {what} must be [rows, heads, D] with contiguous last dimension, like q")
-    if q.dtype not in types or dtype not in types:
+    if q.dim() != 3 or k.dim() != 3 or positions.dtype != torch.int32 or not positions.is_contiguous():
+        _bad("spec_rotary: q and k must be [rows, heads, D], positions contiguous int32, one value a row")
+    (rows, H, D), (_, kv, _), (q0, q1, q2), (k0, k1, k2), src, device = q.shape, k.shape, q.stride(), k.stride(), q.dtype, q.device
+    to = src if dtype is None else dtype
+    kinds = types.get(src), types.get(to)
+    if None in kinds:
         _bad("spec_rotary: types must be float32, bfloat16 or float16")
-    if positions.dtype != torch.int32 or positions.numel() != rows or not positions.is_contiguous() or positions.device != q.device:
-        _bad("spec_rotary: positions must be a contiguous int32 tensor, one value a row")
-    if table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous() or table.device != q.device:
+    if k.shape != (rows, kv, D) or k.dtype != src or q2 != 1 or k2 != 1 or k.device != device or positions.numel() != rows or positions.device != device:
+        _bad("spec_rotary: k must be [rows, heads, D] with contiguous last dimension, like q, positions one value a row on the same device")
+    kvv = v0 = v1 = v_at = vo_at = 0
+    vo = None
+    if v is not None:
+        if v.dim() != 3 or v.shape[0] != rows or v.shape[2] != D or v.dtype != src or v.device != device or v.stride(2) != 1:
+            _bad("spec_rotary: v must be [rows, heads, D] with contiguous last dimension, like q")
+        kvv, (v0, v1, _), v_at = v.shape[1], v.stride(), v.data_ptr()
+        vo = torch.empty((rows, kvv, D), dtype=to, device=device)
+        vo_at = vo.data_ptr()
+    if table.dim() != 3 or table.shape[2] != 2 or table.dtype != torch.float32 or not table.is_contiguous() or table.device != device:
         _bad("spec_rotary: table must be a contiguous float32 tensor [span, rot / 2, 2]")
-    H, kv, kvv, device = q.shape[1], k.shape[1], v.shape[1] if v is not None else 0, q.device
-    qo = torch.empty((rows, H, D), dtype=dtype, device=device)
-    ko = torch.empty((rows, kv, D), dtype=dtype, device=device)
-    vo = torch.empty((rows, kvv, D), dtype=dtype, device=device) if v is not None else None
-    qs, ks, vs = q.stride(), k.stride(), v.stride() if v is not None else (0, 0)
-    a = _RotaryArgs(q.data_ptr(), k.data_ptr(), v.data_ptr() if v is not None else None, qo.data_ptr(), ko.data_ptr(), vo.data_ptr() if v is not None else None, positions.data_ptr(),
-                    table.data_ptr(), qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], types[q.dtype], types[dtype], rows, H, kv, kvv, D, 2 * table.shape[1], table.shape[0], int(interleaved))
-    rc = lib.spec_rotary(C.addressof(a), raw_stream(device.index))
+    qo = torch.empty((rows, H, D), dtype=to, device=device)
+    ko = torch.empty((rows, kv, D), dtype=to, device=device)
+    span, half, _ = table.shape
+    rc = lib.spec_rotary(_pack_rotary(q.data_ptr(), k.data_ptr(), v_at, qo.data_ptr(), ko.data_ptr(), vo_at, positions.data_ptr(), table.data_ptr(), q0, q1, k0, k1, v0, v1, *kinds, rows, H, kv, kvv, D,
+                                      2 * half, span, interleaved), raw_stream(device.index))
     if rc:
         _raise(rc)
     return qo, ko, vo

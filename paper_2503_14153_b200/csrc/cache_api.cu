@@ -1,7 +1,9 @@
 // C ABI of the 8-bit paged cache: argument checks and launches. All work is enqueued on the caller's stream; nothing is allocated,
 // nothing waits. Device-side findings (a page or sequence number out of range) go to the cache's status word.
-#include <stdio.h>
 #include <stdarg.h>
+#include <stdio.h>
+
+#include <atomic>
 
 #include "cache_attention.cuh"
 #include "cache_common.cuh"
@@ -80,14 +82,24 @@ AttnShape attn_shape(const spec_cache* c, int n_heads, int max_rows) {
   s.bytes = s.parts + (size_t)(s.mt == 8 ? CAF_CTAS : CAM_SMS) * 2 * s.mt * (c->head_dim + 2) * 4;
   return s;
 }
-template <typename K> int launch_attn(K kernel, int threads, size_t smem, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st, int ctas = CAM_SMS) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return launched("spec_cache_attention: shared memory");
-  kernel<<<ctas, threads, smem, st>>>(a, pl);
+// Leave for a kernel's dynamic shared memory, once a device (the call takes as long as a launch).
+template <auto KERNEL> bool allow_smem(size_t bytes) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  if (dev < 64 && done.load(std::memory_order_relaxed) >> dev & 1) return true;
+  if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+  if (dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return true;
+}
+template <auto KERNEL> int launch_attn(int threads, size_t smem, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st, int ctas = CAM_SMS) {
+  if (!allow_smem<KERNEL>(smem)) return launched("spec_cache_attention: shared memory");
+  KERNEL<<<ctas, threads, smem, st>>>(a, pl);
   return launched("spec_cache_attention");
 }
 // The tcgen05 kernel and, launched ahead of its end, the one that joins the parts of units that it cut.
 template <typename T, int D, int FMT, int ROWS> int launch_umma(const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
-  if (int rc = launch_attn(cache_attention_umma<T, D, FMT, ROWS>, CU_THREADS, cu_smem(D, ROWS), a, pl, st)) return rc;
+  if (int rc = launch_attn<cache_attention_umma<T, D, FMT, ROWS>>(CU_THREADS, cu_smem(D, ROWS), a, pl, st)) return rc;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(pl.nb * pl.nrt * a.c.kv, ROWS / CJ_ROWS);
   cfg.blockDim = dim3(CJ_THREADS);
@@ -100,11 +112,11 @@ template <typename T, int D, int FMT, int ROWS> int launch_umma(const CacheAttnA
   cudaLaunchKernelEx(&cfg, cache_join_kernel<T, D, ROWS>, a, pl);
   return launched("spec_cache_attention: join");
 }
-template <typename T, int D, int FMT> int launch_attn(int mt, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
+template <typename T, int D, int FMT> int launch_rows(int mt, const CacheAttnArgs& a, const CamPlan& pl, cudaStream_t st) {
   switch (mt) {
-    case 8: return launch_attn(cache_attention_few<T, D, FMT>, CAF_THREADS, (size_t)CAF_WARPS * CAF_ROWS * (D + 8) * 4, a, pl, st, CAF_CTAS);
-    case 16: return launch_attn(cache_attention_mma<T, D, FMT, 1>, CAM_THREADS, cam_smem(D), a, pl, st);
-    case 32: return launch_attn(cache_attention_mma<T, D, FMT, 2>, CAM_THREADS, cam_smem(D), a, pl, st);
+    case 8: return launch_attn<cache_attention_few<T, D, FMT>>(CAF_THREADS, (size_t)CAF_WARPS * CAF_ROWS * (D + 8) * 4, a, pl, st, CAF_CTAS);
+    case 16: return launch_attn<cache_attention_mma<T, D, FMT, 1>>(CAM_THREADS, cam_smem(D), a, pl, st);
+    case 32: return launch_attn<cache_attention_mma<T, D, FMT, 2>>(CAM_THREADS, cam_smem(D), a, pl, st);
     case 64: return launch_umma<T, D, FMT, 64>(a, pl, st);
     case 128: return launch_umma<T, D, FMT, 128>(a, pl, st);
     default: return launch_umma<T, D, FMT, 256>(a, pl, st);
@@ -188,7 +200,7 @@ int spec_cache_store(const spec_cache* c, const spec_store_args* r, void* cuda_s
     by_type(r->type, [&](auto t) {
       auto kernel = cache_store_kernel<decltype(t), decltype(d)::value, decltype(f)::value>;
       const int smem = 2 * STORE_WARPS * (int)sizeof(StoreRoom<decltype(t), decltype(d)::value>);
-      if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (smem > 48 * 1024 && !allow_smem<cache_store_kernel<decltype(t), decltype(d)::value, decltype(f)::value>>(smem)) return;
       kernel<<<grid, 32 * STORE_WARPS, smem, st>>>(a);
     });
   });
@@ -304,7 +316,7 @@ int spec_cache_attention(const spec_cache* c, const spec_attention_args* r, void
         auto go = [&](auto t) {
           typedef decltype(t) T;
           constexpr int D = decltype(d)::value, F = decltype(f)::value;
-          return launch_attn<T, D, F>(sh.mt, a, pl, st);
+          return launch_rows<T, D, F>(sh.mt, a, pl, st);
         };
         return r->type == SPEC_TYPE_BF16 ? go(bf16{}) : go(f16{});
       });
