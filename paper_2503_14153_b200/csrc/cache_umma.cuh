@@ -689,9 +689,9 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   }
 }
 
-// Adds the parts of the units that were cut, in the order of their CTAs: a block 16 rows of a unit. In a kernel of its own all SMs take part; the last CTA of a unit alone took 8 us for five
+// Adds the parts of the units that were cut, in the order of their CTAs: a block 8 rows of a unit. In a kernel of its own all SMs take part; the last CTA of a unit alone took 8 us for five
 // parts of 64 rows, 25 for eighteen of 128.
-constexpr int CJ_THREADS = 128, CJ_ROWS = 16;
+constexpr int CJ_THREADS = 128, CJ_ROWS = 8;
 template <typename T, int D, int MT>
 __global__ void __launch_bounds__(CJ_THREADS) cache_join_kernel(CacheAttnArgs a, CamPlan pl) {
   pdl_wait();
@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(CJ_THREADS) cache_join_kernel(CacheAttnArgs a,
     sum[j] = 0.f;
     v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
-#pragma unroll 4
+#pragma unroll 6
   for (int k = c0; k <= c1; ++k) {
     const float* in = pl.part + ((size_t)k * 2 + (k == c0 ? 1 : 0)) * ((size_t)MT * (D + 2));    // (the slots of CamList::part)
     float2 e[RB];
