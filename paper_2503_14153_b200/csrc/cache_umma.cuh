@@ -26,9 +26,9 @@ constexpr int CU_NEW = 128;                                   // rows of the pas
 template <typename T> __host__ __device__ constexpr float cu_raise() { return std::is_same<T, bf16>::value ? 1.1529215046068470e18f : 256.f; }
 
 __host__ __device__ constexpr int cu_v_stages(int ROWS) { return ROWS == 256 ? 1 : 2; }
-__host__ __device__ constexpr size_t cu_smem(int D, int ROWS) {
-  return 1024 + (size_t)((ROWS == 256 ? 2 : 1) /*Q*/ + 2 /*K*/ + cu_v_stages(ROWS)) * 128 * D * 2 + 2 * (size_t)256 * D /*codes*/;
-}
+// Room of q, which the output goes through, too: 32 dims of 128 rows of both groups with 128 and 256 rows a CTA, all dims of 64 rows else
+__host__ __device__ constexpr int cu_q_bytes(int D, int ROWS) { return ROWS == 64 ? 128 * D * 2 : ROWS == 256 && D == 128 ? 2 * 128 * D * 2 : 2 * 128 * 32 * 4; }
+__host__ __device__ constexpr size_t cu_smem(int D, int ROWS) { return 1024 + cu_q_bytes(D, ROWS) + (size_t)(2 /*K*/ + cu_v_stages(ROWS)) * 128 * D * 2 + 2 * (size_t)256 * D /*codes*/; }
 
 // D[tmem] (+)= A[tmem] * B[smem]
 __device__ __forceinline__ void tc_mma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -81,7 +81,8 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
   __shared__ uint32_t tmem_slot;
   const uint32_t raw = smem_u32(smem_raw);
   uint8_t* q_s = smem_raw + (((raw + 1023u) & ~1023u) - raw);
-  uint8_t* k_s0 = q_s + NQ * OPER;                             // [2]
+  static_assert(cu_q_bytes(D, ROWS) >= NQ * OPER && cu_q_bytes(D, ROWS) >= (ROWS == 64 ? 64 * D * 4 : 2 * 128 * 32 * 4), "q and the output's rows fit");
+  uint8_t* k_s0 = q_s + cu_q_bytes(D, ROWS);                   // [2]
   uint8_t* v_s0 = k_s0 + 2 * OPER;                             // [VS]
   uint8_t* code_s = v_s0 + VS * OPER;                          // [CS]
   uint64_t *code_full = bars, *code_empty = bars + 2, *k_full = bars + 4, *k_empty = bars + 6, *v_full = bars + 8, *v_empty = bars + 10, *s_full = bars + 12, *p_full = bars + 14, *q_full = bars + 16,

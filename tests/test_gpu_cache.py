@@ -252,6 +252,28 @@ def test_attention_many_tiles_a_cta(torch, batch, heads, kv, D, n, rows, mask, f
     assert ((lse - wl).abs() <= 2.0 ** -14).all()
 
 
+@pytest.mark.parametrize("batch,heads,kv,rows,n", [(4500, 4, 1, 1, 9), (300, 1, 1, 40, 20), (270, 2, 1, 50, 3), (4200, 1, 1, 12, 2)])
+def test_attention_more_sequences_than_a_launch_deals(torch, batch, heads, kv, rows, n):
+    from paper_2503_14153_b200 import SpecCache
+    g = torch.Generator(device="cuda").manual_seed(batch)
+    dev = SpecCache(1, kv, 64, 2 * batch, batch, 2)
+    for b0 in range(0, batch, 1000):
+        m = min(1000, batch - b0)
+        seqs = torch.arange(b0, b0 + m, dtype=torch.int32, device="cuda")
+        dev.reserve(torch.full((m,), n, dtype=torch.int32, device="cuda"), seqs=seqs)
+    dev.codes.copy_(torch.randint(1, 256, dev.codes.shape, generator=g, device="cuda", dtype=torch.uint8))
+    dev.codes[dev.codes == 0x80] = 1
+    dev.scales.copy_(torch.rand(dev.scales.shape, generator=g, device="cuda") * 0.03 + 1e-3)
+    q, k, v = (torch.randn((batch * rows, h, 64), generator=g, device="cuda").bfloat16() for h in (heads, kv, kv))
+    out = dev.attention(0, q, k, v, batch=batch)
+    dev.check()
+    want = dev.attention(0, q.float(), k.float(), v.float(), batch=batch)
+    # cached values are at most 4.0 in size and nearly all of the rows' below 4.2, and so are their weighted means; rounding of weights and results to bf16
+    assert ((out.float() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -7 * 4.2).all()
+    spread = (out.float() - want).square().mean().sqrt() / want.square().mean().sqrt()
+    assert spread <= 2.0 ** -7
+
+
 def test_attention_calls_of_other_sizes_share_a_workspace(torch):
     rng = np.random.default_rng(21)
     c = _filled(rng, 1, 4, 128, [700, 90, 1500], "int8")
