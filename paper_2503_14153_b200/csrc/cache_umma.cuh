@@ -21,9 +21,10 @@ constexpr int CU_WARPS = CU_SOFT + CU_CONV + 2, CU_THREADS = 32 * CU_WARPS;   //
 constexpr int CU_PAIRS = 256;                                 // (sequence, row tile) pairs a launch can deal
 constexpr int CU_UNIT = 4;                                    // a unit's fixed cost, in tiles
 constexpr int CU_NEW = 128;                                   // rows of the pass a tile
-// What 16 keys may weigh together before the reference is raised. bf16 weights and float32 sums lose nothing at any size (raising at 128: 313 us for a prompt that takes 250); float16 weights, up to
-// 2^7 times this with the rows of the pass, stay below 2^15.
-template <typename T> __host__ __device__ constexpr float cu_raise() { return std::is_same<T, bf16>::value ? 1.1529215046068470e18f : 256.f; }
+// What 16 keys may weigh together before the reference is raised, and how far below the largest key it is set (log2). bf16 weights and float32 sums lose nothing at any size (raising at 128: 313 us for a
+// prompt that takes 280). float16 weights start at 2^6, which leaves them 30 bits down to zero, and stay below 2^13, with the rows of the pass, whose scale c is at least 1.
+template <typename T> __host__ __device__ constexpr float cu_raise() { return std::is_same<T, bf16>::value ? 1.1529215046068470e18f : 8192.f; }
+template <typename T> __host__ __device__ constexpr float cu_lift() { return std::is_same<T, bf16>::value ? 0.f : 6.f; }
 
 __host__ __device__ constexpr int cu_v_stages(int ROWS) { return ROWS == 256 ? 1 : 2; }
 // Room of q, which the output goes through, too: 32 dims of 128 rows of both groups with 128 and 256 rows a CTA, all dims of 64 rows else
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
       if (n > 0 && u.tile1 > u.cached) {
         const int page = c.page(u.s, 0);
         const float f = page >= 0 ? c.scales[((layer_heads + u.kvh) * c.n_pages + page) * 2 + 1] * code_unit<FMT>() : 0.f;
-        if (f > 0.f) cv = std::is_same<T, bf16>::value ? f : fmaxf(f, 0.0078125f);   // (float16 weights, up to 2^8 / c, stay below 2^15)
+        if (f > 0.f) cv = std::is_same<T, bf16>::value ? f : fmaxf(f, 1.f);
       }
       const float lgc = __log2f(cv);
       for (int t = ALT ? (T0 ^ grp) & 1 : 0; t < nt; t += ALT ? 2 : 1, ++my_tiles) {
@@ -461,7 +462,7 @@ __global__ void __launch_bounds__(CU_THREADS, 1) cache_attention_umma(CacheAttnA
             }
             // (a page of scale 0 without a key to see gives NaN, which the maximum leaves out)
             const float top = fmaxf(fmaf(m0, f[0], is_new ? lgc : lg[0]), fmaf(m1, f[1], is_new ? lgc : lg[1]));
-            const float m_new = fmaxf(m_ref, top), alpha = m_new > m_ref ? ex2(m_ref - m_new) : 1.f;
+            const float m_new = fmaxf(m_ref, top - cu_lift<T>()), alpha = m_new > m_ref ? ex2(m_ref - m_new) : 1.f;
             m_ref = m_new;
             l_run *= alpha;
             if (my_tiles > 0) {
