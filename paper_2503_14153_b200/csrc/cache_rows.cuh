@@ -1,5 +1,4 @@
-// Rows on their way into the 8-bit paged cache and out of it: rotary positions, quantised store, read-back. All three move
-// each value once and are bound by HBM.
+// Rows on their way into the 8-bit paged cache and out of it: rotary positions, quantised store, read-back. All three move each value once.
 #pragma once
 #include <type_traits>
 
@@ -9,7 +8,8 @@ namespace spec {
 
 // ------------------------------------------------------------------ rotary positions
 // Pair i of a head, (x1, x2) = (x[i], x[i + rot/2]) in the half layout, (x[2i], x[2i+1]) in the interleaved one, turns by the table's
-// angle of the row's position: y1 = x1 c - x2 s, y2 = x2 c + x1 s. Dims from `rot` on, and all of v, are only cast.
+// angle of the row's position: y1 = x1 c - x2 s, y2 = x2 c + x1 s. Dims from `rot` on, and all of v, are only cast. 4096 rows of 48 heads of 128, bf16: 26 us, 3.9 TB/s (35 with 8-byte reads, 30 with four heads in
+// flight and 112 registers).
 constexpr int ROT_THREADS = 128;
 __host__ __device__ constexpr int rot_heads(int V) { return V == 8 ? 2 : 4; }    // heads whose loads a thread has in flight
 
@@ -124,7 +124,8 @@ __global__ void rotary_table_kernel(float2* table, const double* __restrict__ fr
 // Rows path[b][0..count) of sequence b's rows of the pass (rows 0..count without a path) become tokens len - count .. len - 1. A warp has the
 // K or V blocks of STORE_EACH (layer, head, page) one after another: 16 rows in registers, the scale from their largest magnitude by a warp reduction, one write. A page
 // that held tokens before (the first one, where the sequence does not end at a page's end) keeps a scale at least as large, and its older codes are
-// rounded once more where the scale grew. Rows after the sequence's end are written as zeros.
+// rounded once more where the scale grew. Rows after the sequence's end are written as zeros. 2048 rows of 32 heads into 8 layers: 90 us, 4.5 TB/s; the accepted rows of 16 sequences into 32 layers 57 us, of 128 MB 2.3 TB/s: 2 KB
+// blocks, most of whose rows are older, and the look-ups before them.
 struct StoreArgs {
   CacheView c;
   const void *k, *v;                   // [layers][rows][kv][D]
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(32 * STORE_WARPS) cache_store_kernel(StoreArgs
 }
 
 // ------------------------------------------------------------------ read
-// Tokens start[b] .. start[b] + window - 1 of every sequence and layer, decoded; tokens past the sequence's end are zeros. A warp decodes one block.
+// Tokens start[b] .. start[b] + window - 1 of every sequence and layer, decoded; tokens past the sequence's end are zeros. A warp decodes one block. 32 tokens of 16 sequences and 32 layers: 42 us, bound by the 268 MB it writes.
 struct ReadArgs {
   CacheView c;
   void *k, *v;                         // [layers][batch][window][kv][D]
