@@ -157,26 +157,28 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// `mine`: in lane t < 16, the row of the pass that becomes token t of the page, or -1 (zeros)
+// `mine`: in lane t < 16, the row of the pass that becomes token t of the page, or -1 (zeros); tokens held .. live - 1 are new
 template <typename T, int D>
-__device__ __forceinline__ void store_fetch(StoreRoom<T, D>& room, const T* __restrict__ in, long long stride, int mine, bool held, const uint8_t* code, int lane) {
+__device__ __forceinline__ void store_fetch(StoreRoom<T, D>& room, const T* __restrict__ in, long long stride, int mine, int held, int live, const uint8_t* code, int lane) {
   constexpr int N = 16 / (int)sizeof(T), CH = D / N;            // 16-byte chunks of a row
 #pragma unroll
   for (int i = 0; i < CACHE_PAGE * CH / 32; ++i) {
     const int x = lane + 32 * i, t = x / CH, ch = x % CH, r = __shfl_sync(0xffffffffu, mine, t);
-    cp_async16(smem_u32(room.rows + t * StoreRoom<T, D>::ROW + ch * 16), in + (long long)max(r, 0) * stride + ch * N, r >= 0 ? 16 : 0);
+    if (t >= held && t < live) cp_async16(smem_u32(room.rows + t * StoreRoom<T, D>::ROW + ch * 16), in + (long long)max(r, 0) * stride + ch * N, r >= 0 ? 16 : 0);
   }
-  if (held)
+  if (held > 0)
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) cp_async16(smem_u32(room.codes + (lane + 32 * i) * 16), code + (lane + 32 * i) * 16, 16);
   cp_async_commit();
 }
 
-// One block of K (WHICH 0) or V (1) out of shared memory; tokens before `held` were there before, with scale `was`. Of the block's 16-byte chunks a lane has D / 32: of K number lane + 32 i, 16 dims of a
+// One block of K (WHICH 0) or V (1) out of shared memory; tokens before `held` were there before, with scale `was`, those from `live` on are not there (their rows in shared memory are whatever was). FULL: 16 new tokens,
+// without the questions (a prompt's 2048 rows into 8 layers 90 us instead of 108; the other way, accepted paths of a few tokens, 57 us without them and 44 with). Of the block's 16-byte chunks a lane has D / 32: of K number lane + 32 i, 16 dims of a
 // token; of V dims 2 lane + 64 (i / 2) + i % 2, all tokens of a dim.
-template <typename T, int D, int FMT, int WHICH>
-__device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int held, float was, uint4* code, float* scale, int lane) {
+template <typename T, int D, int FMT, int WHICH, bool FULL>
+__device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int held_, int live_, float was, uint4* code, float* scale, int lane) {
   constexpr int CH = D / 32, N = 16 / (int)sizeof(T), ROW = StoreRoom<T, D>::ROW;
+  const int held = FULL ? 0 : held_, live = FULL ? CACHE_PAGE : live_;
   // largest finite magnitude. 16-bit types: as integers, two at a time; only where that finds an infinity or NaN value by value
   float top = 0.f;
   bool clean = true;
@@ -185,7 +187,9 @@ __device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int hel
 #pragma unroll
     for (int i = 0; i < CACHE_PAGE * D / N / 32; ++i) {
       const int x = lane + 32 * i;
-      const uint4 v = *reinterpret_cast<const uint4*>(room.rows + x / (D / N) * ROW + x % (D / N) * 16);
+      if (i * 32 / (D / N) >= live) break;
+      uint4 v = make_uint4(0u, 0u, 0u, 0u);
+      if (x / (D / N) >= held && x / (D / N) < live) v = *reinterpret_cast<const uint4*>(room.rows + x / (D / N) * ROW + x % (D / N) * 16);
       m = __vmaxu2(__vmaxu2(m, v.x & 0x7fff7fffu), __vmaxu2(v.y & 0x7fff7fffu, __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
     }
     const uint32_t most = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
@@ -197,7 +201,8 @@ __device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int hel
     top = 0.f;
     bool odd = false;
 #pragma unroll 1
-    for (int x = lane; x < CACHE_PAGE * D / N; x += 32) {
+    for (int x = lane + held * (D / N) / 32 * 32; x < live * (D / N); x += 32) {
+      if (x / (D / N) < held) continue;
       const Vec<T, N> v = *reinterpret_cast<const Vec<T, N>*>(room.rows + x / (D / N) * ROW + x % (D / N) * 16);
 #pragma unroll
       for (int e = 0; e < N; ++e) {
@@ -228,8 +233,9 @@ __device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int hel
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int j = lane + 32 * i, t = (j / (D / 2)) * 8 + (j & 7), d = ((j >> 3) % (D / 16)) * 16;
-      uint32_t w[4];
-      if (t < held) {
+      uint32_t w[4] = {0u, 0u, 0u, 0u};
+      if (t >= live) {
+      } else if (t < held) {
         const uint4 o = older[j];
         w[0] = renew(o.x);
         w[1] = renew(o.y);
@@ -256,6 +262,9 @@ __device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int hel
       uint32_t w[2][4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
+        w[0][u] = w[1][u] = 0u;
+        if (2 * u >= live) continue;                 // (tokens 2 u, 2 u + 1, 2 u + 8, 2 u + 9 are at these four places)
+        const uint32_t there = 0xffu | (2 * u + 1 < live ? 0xff00u : 0u) | (2 * u + 8 < live ? 0xff0000u : 0u) | (2 * u + 9 < live ? 0xff000000u : 0u);
         float f[2][4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -266,9 +275,8 @@ __device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int hel
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          w[h][u] = encode(f[h]);
+          w[h][u] = encode(f[h]) & there;
           if (held > 0) {
-            // tokens 2 u, 2 u + 1, 2 u + 8, 2 u + 9 are at these four places
             const uint32_t keep = (2 * u < held ? 0xffu : 0u) | (2 * u + 1 < held ? 0xff00u : 0u) | (2 * u + 8 < held ? 0xff0000u : 0u) | (2 * u + 9 < held ? 0xff000000u : 0u);
             w[h][u] = (w[h][u] & ~keep) | (renew(reinterpret_cast<const uint32_t*>(older + j + h)[u]) & keep);
           }
@@ -302,7 +310,7 @@ __global__ void __launch_bounds__(32 * STORE_WARPS) cache_store_kernel(StoreArgs
     if (r >= r0 && r < r1) mine = r;
     else set_status(c.status, ST_BOUNDS, 203, i);
   }
-  const int each = STORE_WARPS * a.each, warp = threadIdx.x >> 5, held = max(0, first - base), end = min(2 * c.kv, ((int)blockIdx.y + 1) * each);
+  const int each = STORE_WARPS * a.each, warp = threadIdx.x >> 5, held = max(0, first - base), live = min(CACHE_PAGE, len - base), end = min(2 * c.kv, ((int)blockIdx.y + 1) * each);
   StoreRoom<T, D>* room = reinterpret_cast<StoreRoom<T, D>*>(store_smem) + 2 * warp;
   auto block_of = [&](int unit) { return c.block(a.layer0 + layer, unit >> 1, page, unit & 1); };
   float was[2] = {0.f, 0.f};
@@ -310,7 +318,7 @@ __global__ void __launch_bounds__(32 * STORE_WARPS) cache_store_kernel(StoreArgs
     const T* in = unit & 1 ? static_cast<const T*>(a.v) + layer * a.v_layer + (unit >> 1) * a.v_head : static_cast<const T*>(a.k) + layer * a.k_layer + (unit >> 1) * a.k_head;
     const size_t blk = block_of(unit);
     was[to] = held > 0 ? c.scales[blk] : 0.f;
-    store_fetch<T, D>(room[to], in, unit & 1 ? a.v_row : a.k_row, mine, held > 0, c.codes + blk * (CACHE_PAGE * D), lane);
+    store_fetch<T, D>(room[to], in, unit & 1 ? a.v_row : a.k_row, mine, held, live, c.codes + blk * (CACHE_PAGE * D), lane);
   };
   int unit = blockIdx.y * each + warp, at = 0;
   if (unit < end) fetch(unit, 0);
@@ -326,8 +334,9 @@ __global__ void __launch_bounds__(32 * STORE_WARPS) cache_store_kernel(StoreArgs
     const size_t blk = block_of(unit);
     uint4* code = reinterpret_cast<uint4*>(c.codes + blk * (CACHE_PAGE * D));
     const float w = at ? was[1] : was[0];
-    if (unit & 1) store_block<T, D, FMT, 1>(room[at], held, w, code, c.scales + blk, lane);
-    else store_block<T, D, FMT, 0>(room[at], held, w, code, c.scales + blk, lane);
+    const bool full = held == 0 && live == CACHE_PAGE;
+    if (unit & 1) full ? store_block<T, D, FMT, 1, true>(room[at], held, live, w, code, c.scales + blk, lane) : store_block<T, D, FMT, 1, false>(room[at], held, live, w, code, c.scales + blk, lane);
+    else full ? store_block<T, D, FMT, 0, true>(room[at], held, live, w, code, c.scales + blk, lane) : store_block<T, D, FMT, 0, false>(room[at], held, live, w, code, c.scales + blk, lane);
     __syncwarp();                        // (the room is fetched into again)
   }
 }
