@@ -124,8 +124,8 @@ __global__ void rotary_table_kernel(float2* table, const double* __restrict__ fr
 // Rows path[b][0..count) of sequence b's rows of the pass (rows 0..count without a path) become tokens len - count .. len - 1. A warp has the
 // K or V blocks of STORE_EACH (layer, head, page) one after another: 16 rows in registers, the scale from their largest magnitude by a warp reduction, one write. A page
 // that held tokens before (the first one, where the sequence does not end at a page's end) keeps a scale at least as large, and its older codes are
-// rounded once more where the scale grew. Rows after the sequence's end are written as zeros. 2048 rows of 32 heads into 8 layers: 90 us, 4.5 TB/s; the accepted rows of 16 sequences into 32 layers 57 us, of 128 MB 2.3 TB/s: 2 KB
-// blocks, most of whose rows are older, and the look-ups before them.
+// rounded once more where the scale grew. Rows after the sequence's end are written as zeros. 2048 rows of 32 heads into 8 layers: 76 us, 5.3 TB/s; the accepted rows of 16 sequences into 32 layers 49 us, 92 MB:
+// 2 KB blocks of a few rows each, a warp's eight one after another behind four look-ups, in two waves of 16 warps an SM.
 struct StoreArgs {
   CacheView c;
   const void *k, *v;                   // [layers][rows][kv][D]
@@ -173,7 +173,7 @@ __device__ __forceinline__ void store_fetch(StoreRoom<T, D>& room, const T* __re
 }
 
 // One block of K (WHICH 0) or V (1) out of shared memory; tokens before `held` were there before, with scale `was`, those from `live` on are not there (their rows in shared memory are whatever was). FULL: 16 new tokens,
-// without the questions (a prompt's 2048 rows into 8 layers 90 us instead of 108; the other way, accepted paths of a few tokens, 57 us without them and 44 with). Of the block's 16-byte chunks a lane has D / 32: of K number lane + 32 i, 16 dims of a
+// without the questions (a prompt's 2048 rows into 8 layers 76 us, with them 108; accepted paths of a few tokens 57 us without them, 49 with both forms in the kernel). Of the block's 16-byte chunks a lane has D / 32: of K number lane + 32 i, 16 dims of a
 // token; of V dims 2 lane + 64 (i / 2) + i % 2, all tokens of a dim.
 template <typename T, int D, int FMT, int WHICH, bool FULL>
 __device__ __forceinline__ void store_block(const StoreRoom<T, D>& room, int held_, int live_, float was, uint4* code, float* scale, int lane) {
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(32 * STORE_WARPS) cache_store_kernel(StoreArgs
 }
 
 // ------------------------------------------------------------------ read
-// Tokens start[b] .. start[b] + window - 1 of every sequence and layer, decoded; tokens past the sequence's end are zeros. A warp decodes one block. 32 tokens of 16 sequences and 32 layers: 42 us, bound by the 268 MB it writes.
+// Tokens start[b] .. start[b] + window - 1 of every sequence and layer, decoded; tokens past the sequence's end are zeros. A warp decodes one block. 16 tokens of 16 sequences and 32 layers: 42 us, 4.8 TB/s; 2048 of 8 layers 78 us, 5.2.
 struct ReadArgs {
   CacheView c;
   void *k, *v;                         // [layers][batch][window][kv][D]
