@@ -33,7 +33,6 @@ struct CacheView {
   float* scales;
   int *page_table, *refs, *lens, *status;
   int n_layers, kv, D, n_pages, max_seqs, pages_per_seq;
-  __device__ __host__ __forceinline__ int block_bytes() const { return CACHE_PAGE * D; }
   // number of the (layer, head, page, K|V) block
   __device__ __host__ __forceinline__ size_t block(int layer, int head, int page, int which) const {
     return ((((size_t)layer * kv + head) * n_pages + page) * 2 + which);
